@@ -169,6 +169,59 @@ int medusa_pack_weight(int dtype, const void* src, int64_t n_rows, int64_t k, vo
 int medusa_pack_weight_bf16_as_f16(const void* src, int64_t n_rows, int64_t k, void* dst, int64_t dst_rows,
                                    int64_t tile_offset, int64_t tile_stride, void* stream);
 
+/* ---- 8-bit integer products ----------------------------------------------------------------- */
+
+/* Rows and weights in 8 bits, and the products of a decoder layer on them.  A row t in 8 bits is one signed 8-bit code
+ * per element and one fp32 scale: scale = max|t| / 127 (1 where that is zero), code = the integer nearest to t / scale,
+ * ties to even, clamped to +-127, decided in fp32; it stands for code * scale.  A row that holds a NaN or an infinity
+ * gets the scale NaN and codes 0 (whatever is computed from it is NaN).  Activations have a scale per row (token),
+ * weights one per output feature.  Rows are contiguous and may start anywhere; scales must be 4-byte aligned and
+ * 16- and 32-bit elements aligned to their size.  Widths, row counts and numbers of output features are free (0 rows:
+ * nothing is enqueued); inputs and outputs must not overlap except where a parameter says so.  */
+
+#define MDZ_I8_TILE_ROWS 16 /* rows per tile of a packed 8-bit matrix */
+
+/* Bytes of a packed 8-bit [n_rows, k] matrix with its scales (k <= 131071: no 32-bit sum can overflow). */
+int64_t medusa_packed_i8_bytes(int64_t n_rows, int64_t k);
+
+/* Quantises a ROW-MAJOR [n_rows, k] matrix of any storage dtype, one scale per row (output feature), into rows
+ * 16 * tile_offset .. of `dst`, a packed matrix of dst_rows rows in total that starts on 16 bytes: matrices are stacked
+ * (wqkv: Wq, Wk, Wv; wgateup of an 8-bit model: Wgate, then Wup).  n_rows must be a multiple of 16 unless this is the
+ * last matrix of the stack. */
+int medusa_pack_weight_i8(int dtype, const void* src, int64_t n_rows, int64_t k, void* dst, int64_t dst_rows,
+                          int64_t tile_offset, void* stream);
+
+/* The same for a matrix that is in 8 bits already: ROW-MAJOR codes [n_rows, k] and scales [n_rows]. */
+int medusa_pack_codes_i8(const int8_t* codes, const float* scales, int64_t n_rows, int64_t k, void* dst, int64_t dst_rows,
+                         int64_t tile_offset, void* stream);
+
+/* src [rows, d] of type dtype -> codes [rows, d], scales [rows]; values_opt (nullable, here and below): [rows, d] of
+ * type dtype, what the codes stand for. */
+int medusa_quantize_rows_i8(int dtype, const void* src, int rows, int d, int8_t* codes, float* scales, void* values_opt,
+                            void* stream);
+
+/* The residual's addition and RMSNorm with an output in 8 bits: x' = x + delta (fp32), y = x' * gain *
+ * rsqrt(mean(x'^2) + eps), codes and scales of the rows of y.  (The codes are those of x' * gain: the factor is
+ * positive and goes into the scale alone.)  x [rows, d] fp32; delta_opt (nullable) [rows, d], fp32 or of type dtype, as
+ * delta_dtype says; gain [d] and values_opt of type dtype; x_out_opt (nullable) [rows, d] fp32 receives x' and may be x
+ * itself. */
+int medusa_residual_rmsnorm_i8(int dtype, const float* x, const void* delta_opt, int delta_dtype, const void* gain,
+                               float eps, int rows, int d, float* x_out_opt, int8_t* codes, float* scales,
+                               void* values_opt, void* stream);
+
+/* gate_up [rows, 2 * ffn] of type dtype, a row's gate then its up columns: codes and scales of the rows of
+ * SiLU(gate) * up [rows, ffn]. */
+int medusa_swiglu_i8(int dtype, const void* gate_up, int rows, int ffn, int8_t* codes, float* scales, void* values_opt,
+                     void* stream);
+
+/* y[m][n] = scales[m] * scale of row n * sum_k codes[m][k] * code[n][k]: codes [M, K], y [M, N] of type out_dtype,
+ * packed: an 8-bit [N, K] matrix as above.  The sums are exact in 32-bit integers; a result does not depend on M or on
+ * the order of the sums.  ws: medusa_linear_i8_workspace_bytes(M, N, K) bytes of scratch (0: ws may be NULL); nothing in
+ * it has to be set, and nothing is kept in it. */
+int64_t medusa_linear_i8_workspace_bytes(int M, int N, int K);
+int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, int out_dtype,
+                     void* y, void* ws, int64_t ws_bytes, void* stream);
+
 /* ---- KV cache ------------------------------------------------------------------------------- */
 
 /* Bytes of EACH of desc->k and desc->v (negative = mdz_status). */

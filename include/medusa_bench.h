@@ -24,7 +24,7 @@ int medusa_profile_begin(int max_launches);
 /* Stops recording, waits for the recorded events, and writes one text line per kernel family into the HOST
  * buffer `report`: "name,launches,total_us,min_us,max_us\n" (families: gemm_w64 / gemm_n64 / gemm_w32 /
  * gemm_n32 = the weight-streaming GEMM instantiated for 128- or 64-column bands and 64 or <= 32 rows,
- * gemm_portable, gemm_large, attention, rmsnorm, rope, swiglu, embed, select, accept, kv_compact, misc). */
+ * gemm_portable, gemm_large, gemm_i8, attention, rmsnorm, rows_i8, rope, swiglu, embed, select, accept, kv_compact, misc). */
 int medusa_profile_end(char* report, int64_t report_bytes);
 
 /* ---- calibration streams ----------------------------------------------------------------------------- */

@@ -1,0 +1,45 @@
+// Rows in 8-bit integers (include/medusa.h, "8-bit integer products"): the quantiser that every kernel writing such rows shares, and
+// the packed layout of 8-bit weights.
+#pragma once
+#include "kernels.h"
+
+namespace mdz {
+
+// ---- rows ------------------------------------------------------------------------------------------
+// A row t in 8 bits: scale = max|t| / 127 (1 where that is zero), code = the integer nearest to t / scale, ties to even, clamped to
+// +-127; decided in fp32.  A row that holds a NaN or an infinity has no scale: it becomes NaN and the codes 0, so that everything
+// computed from the row is NaN, as it would be from the row itself.
+constexpr float kI8Max = 127.f;
+// max|t| is kept as its bits: as integers, the magnitudes of fp32 numbers order as the numbers do, then infinity, then NaN
+__device__ inline uint32_t abs_bits(float t) { return __float_as_uint(t) & 0x7FFFFFFFu; }
+struct I8Quantiser {
+  float scale;
+  bool bad;
+  __device__ explicit I8Quantiser(uint32_t amax_bits) {
+    bad = amax_bits >= 0x7F800000u;
+    const float s = __uint_as_float(amax_bits) / kI8Max;
+    scale = bad ? __uint_as_float(0x7FC00000u) : s > 0.f ? s : 1.f;
+  }
+  __device__ inline float round(float t) const {  // the code, as a number
+    return bad ? 0.f : fminf(fmaxf(rintf(t / scale), -kI8Max), kI8Max);
+  }
+};
+
+// ---- packed weights --------------------------------------------------------------------------------
+// Rows (output features) in tiles of 16, input features in k-steps of 64.  Memory order [tile][k-step][lane][16 codes]: one k-step of a
+// tile is 1 KiB, the B operand of v_mfma_i32_16x16x64_i8 (lane l: row l % 16, features 64 ks + 16 (l / 16) .. +15), so a wave loads it
+// with one instruction, and a tile is one contiguous stream.  Features are padded to 128 and rows to 16 with zeros.  One fp32 scale per
+// (padded) row follows the codes of the whole matrix.
+constexpr int kI8TileRows = MDZ_I8_TILE_ROWS;
+constexpr int kI8KStep = 64;
+constexpr int kI8MaxK = 131071;  // 128 * 128 * k < 2^31: no sum of products of codes leaves 32 bits
+__host__ __device__ inline int64_t i8_padded_k(int64_t k) { return (k + 127) / 128 * 128; }
+__host__ __device__ inline int64_t i8_padded_rows(int64_t n) { return (n + kI8TileRows - 1) / kI8TileRows * kI8TileRows; }
+__host__ __device__ inline int64_t i8_scales_offset(int64_t n, int64_t k) { return i8_padded_rows(n) * i8_padded_k(k); }  // bytes
+__host__ __device__ inline int64_t i8_packed_bytes(int64_t n, int64_t k) { return i8_scales_offset(n, k) + 4 * i8_padded_rows(n); }
+// byte of (row n, feature k); kp = i8_padded_k
+__host__ __device__ inline int64_t i8_index(int64_t n, int64_t k, int64_t kp) {
+  return (n >> 4) * 16 * kp + (k >> 6) * 1024 + ((n & 15) + 16 * ((k >> 4) & 3)) * 16 + (k & 15);
+}
+
+}  // namespace mdz
