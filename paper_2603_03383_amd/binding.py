@@ -7,6 +7,7 @@ built (``python -c "import __graft_entry__ as g; g.build()"``) importing works b
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -248,42 +249,46 @@ MDZ_I8_TILE_ROWS = 16
 _STORAGE = {torch.bfloat16: MDZ_BF16, torch.float16: MDZ_FP16, torch.float32: MDZ_FP32}
 
 
-def _operand(name: str, t: Optional[torch.Tensor], shape, *dtypes) -> Optional[C.c_void_p]:
-    """Pointer of a tensor that has this shape and one of these types; None stays None."""
+def _operand(name: str, t: Optional[torch.Tensor], shape, dtype) -> Optional[int]:
+    """Address of a tensor that has this shape and type; None stays None."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype not in dtypes:
-        raise MedusaError(-2, f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} of {' or '.join(map(str, dtypes))}")
+    if t.dtype is not dtype or t.shape != shape:
+        raise MedusaError(-2, f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
     if not t.is_contiguous():
         raise MedusaError(-2, f"{name}: tensors handed to the library must be contiguous")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _storage(name: str, t: torch.Tensor) -> int:
-    if t.dim() != 2 or t.dtype not in _STORAGE:
-        raise MedusaError(-2, f"{name}: {tuple(t.shape)} {t.dtype}, expected rows of a storage dtype")
-    return _STORAGE[t.dtype]
+def _rows(name: str, t: torch.Tensor):
+    """(shape, storage dtype) of a tensor of rows."""
+    shape, dtype = t.shape, _STORAGE.get(t.dtype)
+    if len(shape) != 2 or dtype is None:
+        raise MedusaError(-2, f"{name}: {tuple(shape)} {t.dtype}, expected rows of a storage dtype")
+    return shape, dtype
 
 
+@functools.lru_cache(maxsize=None)
 def medusa_packed_i8_bytes(n_rows: int, k: int) -> int:
     return _check(lib().medusa_packed_i8_bytes(n_rows, k))
 
 
-def _packed_i8(dst: torch.Tensor, dst_rows: int, k: int) -> C.c_void_p:
+def _packed_i8(dst: torch.Tensor, dst_rows: int, k: int) -> int:
     if dst.numel() * dst.element_size() < medusa_packed_i8_bytes(dst_rows, k):
         raise MedusaError(-2, f"packed: {dst.numel() * dst.element_size()} bytes are too few for [{dst_rows}, {k}]")
-    return _ptr(dst)
+    return _operand("packed", dst, dst.shape, dst.dtype)
 
 
 def medusa_pack_weight_i8(src: torch.Tensor, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0, stream=None) -> None:
     """src [n, k] of a storage dtype -> rows 16 * tile_offset .. of the packed 8-bit matrix dst, quantised per row."""
-    dtype, (n, k) = _storage("src", src), src.shape
-    _check(lib().medusa_pack_weight_i8(dtype, _operand("src", src, src.shape, src.dtype), n, k, _packed_i8(dst, dst_rows, k), dst_rows, tile_offset,
-                                       _stream(stream)))
+    shape, dtype = _rows("src", src)
+    _check(lib().medusa_pack_weight_i8(dtype, _operand("src", src, shape, src.dtype), shape[0], shape[1],
+                                       _packed_i8(dst, dst_rows, shape[1]), dst_rows, tile_offset, _stream(stream)))
 
 
 def medusa_pack_codes_i8(codes: torch.Tensor, scales: torch.Tensor, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0,
                          stream=None) -> None:
+    """codes int8 [n, k] with scales fp32 [n] -> the same rows of the packed 8-bit matrix dst."""
     n, k = codes.shape
     _check(lib().medusa_pack_codes_i8(_operand("codes", codes, (n, k), torch.int8), _operand("scales", scales, (n,), torch.float32), n, k,
                                       _packed_i8(dst, dst_rows, k), dst_rows, tile_offset, _stream(stream)))
@@ -291,32 +296,33 @@ def medusa_pack_codes_i8(codes: torch.Tensor, scales: torch.Tensor, dst: torch.T
 
 def medusa_quantize_rows_i8(src, codes, scales, values=None, stream=None) -> None:
     """src [rows, d] -> codes int8 [rows, d], scales fp32 [rows]; values (optional, src's type): what they stand for."""
-    dtype, shape = _storage("src", src), src.shape
-    _check(lib().medusa_quantize_rows_i8(dtype, _operand("src", src, shape, src.dtype), shape[0], shape[1], _operand("codes", codes, shape, torch.int8),
-                                         _operand("scales", scales, shape[:1], torch.float32),
-                                         _operand("values", values, shape, src.dtype), _stream(stream)))
+    shape, dtype = _rows("src", src)
+    rows, d = shape
+    _check(lib().medusa_quantize_rows_i8(dtype, _operand("src", src, shape, src.dtype), rows, d, _operand("codes", codes, shape, torch.int8),
+                                         _operand("scales", scales, (rows,), torch.float32), _operand("values", values, shape, src.dtype),
+                                         _stream(stream)))
 
 
 def medusa_residual_rmsnorm_i8(x, delta, gain, eps: float, x_out, codes, scales, values=None, stream=None) -> None:
     """x [rows, d] fp32 (+ delta, fp32 or gain's type, or None) -> x_out (x itself, another, or None) and RMSNorm(x') in 8 bits."""
-    _storage("x", x)
-    shape, td = x.shape, gain.dtype
+    shape, _ = _rows("x", x)
+    rows, d = shape
+    td, td_delta = gain.dtype, torch.float32 if delta is None or delta.dtype is torch.float32 else gain.dtype
     if td not in _STORAGE:
         raise MedusaError(-2, f"gain: {td} is no storage dtype")
     _check(lib().medusa_residual_rmsnorm_i8(
-        _STORAGE[td], _operand("x", x, shape, torch.float32), _operand("delta", delta, shape, torch.float32, td),
-        MDZ_FP32 if delta is None else _STORAGE[delta.dtype], _operand("gain", gain, shape[1:], td), eps, shape[0], shape[1],
-        _operand("x_out", x_out, shape, torch.float32), _operand("codes", codes, shape, torch.int8),
-        _operand("scales", scales, shape[:1], torch.float32), _operand("values", values, shape, td), _stream(stream)))
+        _STORAGE[td], _operand("x", x, shape, torch.float32), _operand("delta", delta, shape, td_delta), _STORAGE[td_delta],
+        _operand("gain", gain, (d,), td), eps, rows, d, _operand("x_out", x_out, shape, torch.float32),
+        _operand("codes", codes, shape, torch.int8), _operand("scales", scales, (rows,), torch.float32),
+        _operand("values", values, shape, td), _stream(stream)))
 
 
 def medusa_swiglu_i8(gate_up, codes, scales, values=None, stream=None) -> None:
     """gate_up [rows, 2 ffn] (gate | up) -> SiLU(gate) * up in 8 bits, codes [rows, ffn]."""
-    dtype, shape = _storage("gate_up", gate_up), codes.shape
-    if len(shape) != 2:
-        raise MedusaError(-2, f"codes: {tuple(shape)}, expected rows")
-    _check(lib().medusa_swiglu_i8(dtype, _operand("gate_up", gate_up, (shape[0], 2 * shape[1]), gate_up.dtype), shape[0], shape[1],
-                                  _operand("codes", codes, shape, torch.int8), _operand("scales", scales, shape[:1], torch.float32),
+    (rows, width), dtype = _rows("gate_up", gate_up)
+    shape = (rows, width // 2)
+    _check(lib().medusa_swiglu_i8(dtype, _operand("gate_up", gate_up, (rows, shape[1] * 2), gate_up.dtype), rows, shape[1],
+                                  _operand("codes", codes, shape, torch.int8), _operand("scales", scales, (rows,), torch.float32),
                                   _operand("values", values, shape, gate_up.dtype), _stream(stream)))
 
 
@@ -326,12 +332,14 @@ def medusa_linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def medusa_linear_i8(codes, scales, packed, y, ws=None, stream=None) -> None:
     """y [M, N] (any storage dtype) = rows (codes [M, K], scales [M]) x the packed 8-bit matrix [N, K], transposed."""
-    out = _storage("y", y)
+    shape, out = _rows("y", y)
+    M, N = shape
     if codes.dim() != 2:
         raise MedusaError(-2, f"codes: {tuple(codes.shape)}, expected rows")
-    (M, K), N = codes.shape, y.shape[1]
+    K = codes.shape[1]
     _check(lib().medusa_linear_i8(_operand("codes", codes, (M, K), torch.int8), _operand("scales", scales, (M,), torch.float32),
-                                  _packed_i8(packed, N, K), M, N, K, out, _operand("y", y, (M, N), y.dtype), _ptr(ws),
+                                  _packed_i8(packed, N, K), M, N, K, out, _operand("y", y, shape, y.dtype),
+                                  None if ws is None else _operand("ws", ws, ws.shape, ws.dtype),
                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
 
 

@@ -1,9 +1,7 @@
 // Product of rows in 8 bits with packed 8-bit weights: y[m][n] = sx[m] * sw[n] * sum_k cx[m][k] * cw[n][k], sums in 32-bit integers.
-#include "i8.h"
+#include "gemm_i8.h"
 
 namespace mdz {
-
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // 16 codes of a row of K from feature k on (any alignment); features beyond K come as zeros
 __device__ inline i32x4 load_codes(const int8_t* row, int k, int K) {
@@ -14,54 +12,144 @@ __device__ inline i32x4 load_codes(const int8_t* row, int k, int K) {
   return v;
 }
 
-// A workgroup of four waves makes MT 16-row tiles x one 16-column tile: the waves share the k-steps and add their sums through LDS.
-template <int MT, typename TO>
-__global__ void __launch_bounds__(256) gemm_i8_kernel(const int8_t* __restrict__ X, const float* __restrict__ sx,
-                                                      const uint8_t* __restrict__ Wp, const float* __restrict__ sw, TO* __restrict__ Y,
-                                                      int M, int N, int K, int64_t kp) {
-  __shared__ i32x4 red[4][MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = blockIdx.y * MT * 16;
-  const int n_steps = (K + kI8KStep - 1) / kI8KStep;
+template <int MT, int NT, int NW, int D, typename TO>
+__global__ void __launch_bounds__(NW * 64) gemm_i8_kernel(I8Product p) {
+  constexpr int kTiles = MT * NT;
+  __shared__ i32x4 red[NW][kTiles][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = blockIdx.y * MT * 16, tile0 = blockIdx.x * NT;
+  const int n_steps = p.K / kI8KStep;  // whole ones
+  const int lo = (int)((int64_t)wave * n_steps / NW), hi = (int)((int64_t)(wave + 1) * n_steps / NW);
   const int8_t* xr[MT];
+  const uint8_t* wr[NT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xr[i] = X + (int64_t)min(row0 + i * 16 + (lane & 15), M - 1) * K;
-  const uint8_t* w = Wp + (int64_t)blockIdx.x * 16 * kp + lane * 16;
-  i32x4 acc[MT];
+  for (int i = 0; i < MT; ++i) xr[i] = p.X + (int64_t)min(row0 + i * 16 + (lane & 15), p.M - 1) * p.ldx + 16 * (lane >> 4);
 #pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = i32x4{0, 0, 0, 0};
-  for (int ks = wave; ks < n_steps; ks += 4) {
-    const i32x4 b = *reinterpret_cast<const i32x4*>(w + (int64_t)ks * 1024);
+  for (int j = 0; j < NT; ++j) wr[j] = p.W + (int64_t)min(tile0 + j, p.n_tiles - 1) * 16 * p.kp + lane * 16;
+  i32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  i32x4 xb[D][MT], wb[D][NT];
+  typedef i32x4 i32x4_any __attribute__((aligned(1)));
+  auto load = [&](int b, int ks) {
+    const int64_t k = min(ks, hi - 1);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) wb[b][j] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wr[j] + k * 1024));
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xb[b][i] = *reinterpret_cast<const i32x4_any*>(xr[i] + k * kI8KStep);
+  };
+  auto multiply = [&](int b) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
-      acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_codes(xr[i], ks * kI8KStep + 16 * (lane >> 4), K), b, acc[i], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = mfma_i8(wb[b][j], xb[b][i], acc[i][j]);
+  };
+  if (lo < hi) {
+#pragma unroll
+    for (int b = 0; b < D; ++b) load(b, lo + b);
+    int s = lo;
+    for (; s + D <= hi; s += D)
+#pragma unroll
+      for (int b = 0; b < D; ++b) {
+        multiply(b);
+        load(b, s + b + D);
+      }
+#pragma unroll
+    for (int b = 0; b < D; ++b)
+      if (s + b < hi) multiply(b);
+  }
+  if (p.K % kI8KStep != 0 && wave == NW - 1) {  // the features behind the last whole k-step
+#pragma unroll
+    for (int j = 0; j < NT; ++j) wb[0][j] = *reinterpret_cast<const i32x4*>(wr[j] + (int64_t)n_steps * 1024);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int k = n_steps * kI8KStep + 16 * (lane >> 4);
+      xb[0][i] = load_codes(xr[i] - 16 * (lane >> 4), k, p.K);
+    }
+    multiply(0);
   }
 #pragma unroll
-  for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
+  for (int t = 0; t < kTiles; ++t) red[wave][t][lane] = acc[t / NT][t % NT];
   __syncthreads();
-  for (int p = threadIdx.x; p < MT * 64; p += 256) {
-    const int i = p >> 6, l = p & 63, col = blockIdx.x * 16 + (l & 15);
-    const i32x4 s = red[0][i][l] + red[1][i][l] + red[2][i][l] + red[3][i][l];
+  for (int q = threadIdx.x; q < kTiles * 64; q += NW * 64) {
+    const int t = q >> 6, l = q & 63;
+    i32x4 sum = red[0][t][l];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int row = row0 + i * 16 + 4 * (l >> 4) + e;
-      if (row < M && col < N) Y[(int64_t)row * N + col] = from_float<TO>((float)s[e] * (sx[row] * sw[col]));
-    }
+    for (int w = 1; w < NW; ++w) sum += red[w][t][l];
+    const int row = row0 + t / NT * 16 + (l & 15), tile = tile0 + t % NT, col = tile * 16 + 4 * (l >> 4);
+    if (row < p.M && tile < p.n_tiles) store_scaled<TO>(p, row, col, sum, p.sx[row]);
   }
 }
 
-template <typename TO>
-static int launch_gemm_i8_t(const int8_t* X, const float* sx, const void* Wp, int M, int N, int K, TO* Y, hipStream_t st) {
-  const int64_t kp = i8_padded_k(K);
-  const float* sw = (const float*)((const char*)Wp + i8_scales_offset(N, K));
-  const unsigned n_tiles = (unsigned)(i8_padded_rows(N) / kI8TileRows);
-  auto run = [&](auto kernel, int rows) {
-    launch_timed(PROF_GEMM_I8, kernel, dim3(n_tiles, (M + rows - 1) / rows), 256, 0, st, X, sx, (const uint8_t*)Wp, sw, Y, M, N, K, kp);
-  };
-  if (M <= 16) run(gemm_i8_kernel<1, TO>, 16);
-  else if (M <= 32) run(gemm_i8_kernel<2, TO>, 32);
-  else run(gemm_i8_kernel<4, TO>, 64);
+template <int MT, int NT, int NW, int D, typename TO>
+static int launch_narrow(const I8Product& p, hipStream_t st) {
+  launch_timed(PROF_GEMM_I8, gemm_i8_kernel<MT, NT, NW, D, TO>, dim3((p.n_tiles + NT - 1) / NT, (p.M + MT * 16 - 1) / (MT * 16)), NW * 64, 0, st, p);
   MDZ_LAUNCH_CHECK();
+  return MDZ_OK;
+}
+
+// Rows that do not start on 16 bytes, again 16 bytes apart and padded (with zeros) to whole k-steps.
+__global__ void __launch_bounds__(256) align_rows_kernel(const int8_t* __restrict__ X, int K, i32x4* __restrict__ out, int64_t chunks, int per_row) {
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (q >= chunks) return;
+  const int64_t row = q / per_row;
+  out[q] = load_codes(X + row * K, (int)(q - row * per_row) * 16, K);
+}
+
+struct I8Plan {
+  int tile;    // of kI8Tiles; -1: the kernel of few rows
+  int splits;  // of the features
+  int64_t aligned_at, bytes;  // workspace: the partial sums, then the rows aligned, where a call needs them
+};
+
+// Up to 16 rows take the kernel above; up to 32 do where neither the rows (K) nor the weights are long, because it loads a row in pieces of
+// 64 bytes, a third slower than the tiles' 128 (us, this kernel / tiles: 24 rows 4096 x 4096 7.0 / 8.9, 32 rows 12288 x 4096 13.1 / 14.2;
+// 22016 x 4096 22.8 / 21.1, 4096 x 11008 16.3 / 14.1).  Beyond, the tile and the number of splits of the least modelled time: a launch, and
+// the longest of what a CU needs for its workgroups, what the chip needs for all, and W from HBM; a split adds a launch and its sums'
+// way to memory and back.  Fitted to 2300 timings (1 .. 2048 rows, 688 x 256 .. 22016 x 4096 and 5120 x 13824): what it picks takes 1.3 %
+// longer than the best of them on average, 13 % at most from 64 rows of 1 MB of weights on.
+static I8Plan plan_i8(int M, int N, int K) {
+  I8Plan best{-1, 1, 0, 0};
+  if (M <= 16 || (M <= 32 && K <= 8192 && (int64_t)N * K <= 1 << 26)) return best;
+  const int n_pad = (int)i8_padded_rows(N), stages = (K + 127) / 128, cus = num_cus();
+  const float hbm = (float)N * K * (1e-6f / 4.9f);
+  float least = 0.f;
+  for (int t = 0; t < kNumI8Tiles; ++t) {
+    const I8Tile& tile = kI8Tiles[t];
+    if (t > 0 && tile.rows >= 2 * M) break;
+    const int64_t blocks = (int64_t)((M + tile.rows - 1) / tile.rows) * ((N + tile.cols - 1) / tile.cols);
+    for (int splits : {1, 2, 3, 4, 6, 8}) {
+      if (splits > 1 && (splits * 4 > stages || blocks * splits > 4 * cus)) break;
+      const int64_t wgs = blocks * splits;
+      const float s = (float)((stages + splits - 1) / splits);
+      float rounds = (float)((wgs + cus - 1) / cus);
+      if (rounds > 1.f && tile.two) rounds *= 0.86f;
+      float us = fmaxf(fmaxf(rounds * s * tile.us_stage, (float)wgs * s * tile.us_all), hbm);
+      if (splits > 1) us += 2.f + (float)splits * M * n_pad * (4e-6f / 2.5f);
+      if (best.tile < 0 || us < least) best.tile = t, best.splits = splits, least = us;
+    }
+  }
+  best.aligned_at = best.splits > 1 ? best.splits * (int64_t)M * n_pad * 4 : 0;
+  best.bytes = best.aligned_at + (int64_t)M * i8_padded_k(K);
+  return best;
+}
+
+template <int MT, typename TO>
+static int launch_few_rows(const I8Product& p, hipStream_t st) {
+  // one 16-column tile per workgroup until every CU has one, then two, then three, whose loads share the rows' (us at 1 row, one / two / three
+  // tiles: 4096 x 4096 4.9 / 5.9 / 7.0; 6144 x 4096, 16 rows 9.1 / 7.3 / 8.4; 22016 x 4096 17.5 / 17.4 / 16.6)
+  const int cus = num_cus();
+  if (p.n_tiles <= cus) return launch_narrow<MT, 1, 4, 4, TO>(p, st);
+  if (p.n_tiles <= 2 * cus) return launch_narrow<MT, 2, 4, 4, TO>(p, st);
+  return launch_narrow<MT, 3, 4, MT == 1 ? 6 : 4, TO>(p, st);
+}
+
+static int check_linear_i8(int M, int N, int K) {
+  MDZ_REQUIRE(M >= 0 && N > 0 && K > 0, MDZ_EINVAL, "linear_i8: [%d,%d] x [%d,%d]", M, K, N, K);
+  MDZ_REQUIRE(K <= kI8MaxK, MDZ_EUNSUPPORTED, "linear_i8: up to %d input features, whose 32-bit sums cannot overflow (%d)", kI8MaxK, K);
+  MDZ_REQUIRE((int64_t)M * N < (int64_t)1 << 40 && N <= INT32_MAX - kI8TileRows, MDZ_EUNSUPPORTED, "linear_i8: %d x %d outputs", M, N);
   return MDZ_OK;
 }
 
@@ -73,24 +161,38 @@ extern "C" {
 #pragma GCC visibility push(default)
 
 int64_t medusa_linear_i8_workspace_bytes(int M, int N, int K) {
-  MDZ_REQUIRE(M >= 0 && N > 0 && K > 0, MDZ_EINVAL, "linear_i8: [%d,%d] x [%d,%d]", M, K, N, K);
-  MDZ_REQUIRE(K <= kI8MaxK, MDZ_EUNSUPPORTED, "linear_i8: up to %d input features, whose 32-bit sums cannot overflow (%d)", kI8MaxK, K);
-  return 0;
+  const int rc = check_linear_i8(M, N, K);
+  return rc ? rc : plan_i8(M, N, K).bytes;
 }
 
 int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, int out_dtype, void* y, void* ws,
                      int64_t ws_bytes, void* stream) {
   MDZ_REQUIRE(dtype_ok(out_dtype), MDZ_EINVAL, "linear_i8: bad dtype %d", out_dtype);
-  const int64_t need = medusa_linear_i8_workspace_bytes(M, N, K);
-  if (need < 0) return (int)need;
+  int rc = check_linear_i8(M, N, K);
+  if (rc) return rc;
   if (M == 0) return MDZ_OK;
   MDZ_REQUIRE(codes && scales && packed && y, MDZ_EINVAL, "linear_i8: NULL pointer");
   MDZ_REQUIRE((reinterpret_cast<uintptr_t>(packed) & 15) == 0, MDZ_EINVAL, "linear_i8: the packed matrix must start on 16 bytes");
   MDZ_REQUIRE(reinterpret_cast<uintptr_t>(scales) % 4 == 0 && reinterpret_cast<uintptr_t>(y) % elem_bytes(out_dtype) == 0, MDZ_EINVAL,
               "linear_i8: a buffer is not aligned to its elements");
-  MDZ_REQUIRE(ws_bytes >= need && (ws || need == 0), MDZ_EWORKSPACE, "linear_i8: workspace %lld < %lld bytes", (long long)ws_bytes,
-              (long long)need);
-  MDZ_WITH_ELEM(out_dtype, return launch_gemm_i8_t<E>(codes, scales, packed, M, N, K, (E*)y, (hipStream_t)stream));
+  const I8Plan plan = plan_i8(M, N, K);
+  MDZ_REQUIRE(ws_bytes >= plan.bytes && (ws || plan.bytes == 0), MDZ_EWORKSPACE, "linear_i8: workspace %lld < %lld bytes",
+              (long long)ws_bytes, (long long)plan.bytes);
+  MDZ_REQUIRE(plan.bytes == 0 || (reinterpret_cast<uintptr_t>(ws) & 15) == 0, MDZ_EINVAL, "linear_i8: the workspace must start on 16 bytes");
+  hipStream_t st = (hipStream_t)stream;
+  I8Product p{};
+  p.X = codes, p.sx = scales, p.W = (const uint8_t*)packed, p.sw = (const float*)((const char*)packed + i8_scales_offset(N, K)), p.Y = y;
+  p.M = M, p.N = N, p.K = K, p.ldx = K, p.kp = i8_padded_k(K), p.n_tiles = (int)(i8_padded_rows(N) / kI8TileRows);
+  p.quads = N % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * elem_bytes(out_dtype)) == 0;
+  if (plan.tile < 0) MDZ_WITH_ELEM(out_dtype, return (M <= 16 ? launch_few_rows<1, E>(p, st) : launch_few_rows<2, E>(p, st)));
+  if (K % 16 != 0 || reinterpret_cast<uintptr_t>(codes) % 16 != 0) {  // the tiles' loads take 16 bytes from addresses of 16
+    i32x4* aligned = (i32x4*)((char*)ws + plan.aligned_at);
+    const int64_t chunks = (int64_t)M * (p.kp / 16);
+    launch_timed(PROF_GEMM_I8, align_rows_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, codes, K, aligned, chunks, (int)(p.kp / 16));
+    MDZ_LAUNCH_CHECK();
+    p.X = (const int8_t*)aligned, p.ldx = p.kp, p.K = (int)p.kp;
+  }
+  return launch_i8_tile(out_dtype, p, plan.tile, plan.splits, ws, st);
 }
 
 #pragma GCC visibility pop

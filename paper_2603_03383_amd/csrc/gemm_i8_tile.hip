@@ -1,0 +1,186 @@
+// Product of 8-bit rows with packed 8-bit weights over more than 16 rows: a workgroup owns a tile of the output, X and W go straight to an
+// LDS ring, v_mfma_i32_16x16x64_i8 multiplies.
+#include "gemm_i8.h"
+#include "gemm_rows.h"
+
+namespace mdz {
+
+
+// all but the youngest `n` stages of L loads each have landed, for n <= NS
+template <int L, int NS>
+__device__ inline void wait_stages(int n) {
+  if (n >= NS) wait_loads<NS * L>();
+  else static_for<NS>([&](auto i) {
+    if (n == decltype(i)::value) wait_loads<decltype(i)::value * L>();
+  });
+}
+
+constexpr int kI8Stage = 128;  // features of a stage of the ring: one cache line of a row of X, two k-steps of a tile of W
+
+// Waves: WR x WC, each with MT 16-row tiles x NT 16-column tiles.  NS stages of the ring.  PARTIAL: a workgroup sums a part of the
+// features (blockIdx.z) and writes its 32-bit sums to P[blockIdx.z], [M][n_tiles * 16].
+template <int WR, int WC, int MT, int NT, int NS, typename TO, bool PARTIAL>
+__global__ void __launch_bounds__(WR * WC * 64) gemm_i8_tile_kernel(I8Product p, i32x4* __restrict__ P, int nb_m, int nb_n, int splits) {
+  constexpr int NW = WR * WC, XT = WR * MT, WT = WC * NT;  // waves; 16-row and 16-column tiles of the workgroup
+  constexpr int UX = XT * 2, U = (XT + WT) * 2;            // 1 KiB pieces of a stage: X (8 rows x 128 features), then W (a k-step of a tile)
+  constexpr int L = (U + NW - 1) / NW;                     // loads per wave and stage (a wave without a piece repeats the last)
+  constexpr uint32_t kSlot = U * 1024;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds_raw[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave / WC, wc = wave % WC;
+  // workgroups go round-robin to the 8 XCDs: the row blocks of a column block follow each other on one of them
+  const int xcd = blockIdx.x & 7, seq = blockIdx.x >> 3;
+  const int bn = (seq / nb_m) * 8 + xcd, bm = seq % nb_m;
+  if (bn >= nb_n) return;
+  const int n_stages = (p.K + kI8Stage - 1) / kI8Stage;
+  const int lo = (int)((int64_t)blockIdx.z * n_stages / splits), n = (int)((int64_t)(blockIdx.z + 1) * n_stages / splits) - lo;
+  const int row0 = bm * XT * 16, tile0 = bn * WT;
+  const int last_row = p.M - 1 - row0, last_tile = p.n_tiles - 1 - tile0;
+  const uint32_t lds0 = MDZ_LDS_ADDR(lds_raw);
+  const uint8_t* x0 = reinterpret_cast<const uint8_t*>(p.X) + (int64_t)row0 * p.ldx + (int64_t)lo * kI8Stage;
+  const uint8_t* w0 = p.W + (int64_t)tile0 * 16 * p.kp + (int64_t)lo * 2048;
+  const uint32_t ldx = (uint32_t)p.ldx, tile_bytes = (uint32_t)p.kp * 16;
+  // A piece of X: row lane / 8 of its eight, and the 16-byte chunk lane % 8, which changes places by the row's number so that the reads
+  // spread over the banks.  Rows beyond M repeat the last and tiles beyond the matrix its last; neither is stored.
+  const int chunk = ((lane & 7) ^ (lane >> 3)) * 16;
+  auto load = [&](int s, int slot) {
+    const uint32_t dst = lds0 + slot * kSlot;
+    // (the last chunk again for those beyond K, whose weights are zero)
+    const int at = min(chunk, p.K - 16 - (lo + s) * kI8Stage);
+    static_for<L>([&](auto i) {
+      constexpr int q = decltype(i)::value, first = q * NW, last = first + NW - 1;
+      const int u = last < U ? first + wave : min(first + wave, U - 1);
+      const uint8_t* const xp = x0 + (int64_t)s * kI8Stage;
+      const uint8_t* const wp = w0 + (int64_t)s * 2048;
+      const uint32_t xo = __umul24(min(u * 8 + (lane >> 3), last_row), ldx) + at;
+      const uint32_t wo = (uint32_t)min((u - UX) >> 1, last_tile) * tile_bytes + ((u & 1) * 1024 + lane * 16);
+      const bool of_x = last < UX || (first < UX && u < UX);
+      load_to_lds<0>(of_x ? xp : wp, of_x ? xo : wo, dst + u * 1024);
+    });
+  };
+  auto read = [&](i32x4(&a)[NT], i32x4(&b)[MT], int slot, int ks) {
+    const uint8_t* xs = lds_raw + slot * kSlot;
+    const uint8_t* ws = xs + UX * 1024;
+    const int r = lane & 15, c = (ks * 4 + (lane >> 4)) ^ (r & 7);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) a[j] = *reinterpret_cast<const i32x4*>(ws + ((wc * NT + j) * 2 + ks) * 1024 + lane * 16);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) b[i] = *reinterpret_cast<const i32x4*>(xs + (wr * MT + i) * 2048 + r * 128 + c * 16);
+  };
+
+  i32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  auto multiply = [&](const i32x4(&a)[NT], const i32x4(&b)[MT]) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = mfma_i8(a[j], b[i], acc[i][j]);
+  };
+
+  static_for<NS>([&](auto i) {
+    if (decltype(i)::value < n) load(decltype(i)::value, decltype(i)::value);
+  });
+  if (n > 0) {
+    i32x4 a0[NT], b0[MT], a1[NT], b1[MT];  // the operands of a k-step are read while the one before multiplies
+    wait_stages<L, NS - 1>(n - 1);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read(a0, b0, 0, 0);
+    int slot = 0;
+    for (int s = 0; s < n; ++s) {
+      read(a1, b1, slot, 1);
+      multiply(a0, b0);
+      const int next = slot + 1 == NS ? 0 : slot + 1;
+      if (s + 1 < n) {
+        wait_lds();
+        wait_stages<L, NS - 2>(n - 2 - s);  // this wave's loads of the next stage have landed, its reads of this one too
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (s + NS < n) load(s + NS, slot);
+        read(a0, b0, next, 0);
+      }
+      multiply(a1, b1);
+      slot = next;
+    }
+  }
+
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int row = row0 + (wr * MT + i) * 16 + (lane & 15);
+    if (row >= p.M) continue;
+    const float sx = PARTIAL ? 0.f : p.sx[row];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int tile = tile0 + wc * NT + j, col = tile * 16 + 4 * (lane >> 4);
+      if (tile >= p.n_tiles) continue;
+      if constexpr (PARTIAL)
+        P[(((int64_t)blockIdx.z * p.M + row) * p.n_tiles * 16 + col) >> 2] = acc[i][j];
+      else
+        store_scaled<TO>(p, row, col, acc[i][j], sx);
+    }
+  }
+}
+
+// y = scaled sum of the partial sums: a thread has four columns of a row
+template <typename TO>
+__global__ void __launch_bounds__(256) gemm_i8_finish_kernel(I8Product p, const i32x4* __restrict__ P, int splits) {
+  const int64_t quads = (int64_t)p.M * p.n_tiles * 4, q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (q >= quads) return;
+  i32x4 s = P[q];
+  for (int z = 1; z < splits; ++z) s += P[z * quads + q];
+  const int row = (int)(q / (p.n_tiles * 4)), col = (int)(q % (p.n_tiles * 4)) * 4;
+  store_scaled<TO>(p, row, col, s, p.sx[row]);
+}
+
+template <int WR, int WC, int MT, int NT, int NS, typename TO, bool PARTIAL>
+static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream_t st) {
+  constexpr int kLds = (WR * MT + WC * NT) * 2048 * NS;
+  const int nb_m = (p.M + WR * MT * 16 - 1) / (WR * MT * 16), nb_n = (p.n_tiles + WC * NT - 1) / (WC * NT);
+  auto kernel = gemm_i8_tile_kernel<WR, WC, MT, NT, NS, TO, PARTIAL>;
+  MDZ_SET_LDS_ONCE(kernel, kLds);
+  launch_timed(PROF_GEMM_I8, kernel, dim3((unsigned)((nb_n + 7) / 8 * 8) * nb_m, 1, splits), WR * WC * 64, kLds, st, p, partial, nb_m, nb_n, splits);
+  MDZ_LAUNCH_CHECK();
+  return MDZ_OK;
+}
+
+// Waves (rows x columns of them), 16-row and 16-column tiles of a wave, stages of the ring, and the two times of I8Tile.  Few rows take wide
+// rings of small stages (a CU's intake is the bound, and two workgroups per CU cover each other's start and end); many rows take the
+// largest tiles, which need the fewest bytes per product.
+#define MDZ_I8_TILES(T)         \
+  T(2, 2, 1, 1, 8, .168, .385)  \
+  T(4, 1, 1, 3, 5, .247, 1.02)  \
+  T(2, 2, 2, 2, 4, .302, 1.03)  \
+  T(4, 3, 1, 2, 4, .364, 1.60)  \
+  T(2, 4, 3, 1, 5, .371, 1.45)  \
+  T(2, 4, 4, 1, 4, .417, 1.73)  \
+  T(2, 4, 4, 2, 4, .624, 2.55)  \
+  T(4, 4, 4, 2, 3, .947, 3.92)  \
+  T(4, 2, 4, 6, 2, 1.307, 6.06)
+#define MDZ_I8_TILE_FACTS(WR, WC, MT, NT, NS, STAGE, ALL) \
+  {WR * MT * 16, WC * NT * 16, (WR * MT + WC * NT) * 2048 * NS <= 80 * 1024, STAGE##f, ALL##f * 1e-3f},
+const I8Tile kI8Tiles[kNumI8Tiles] = {MDZ_I8_TILES(MDZ_I8_TILE_FACTS)};
+
+template <typename TO, bool PARTIAL>
+static int launch_by_tile(const I8Product& p, int tile, int splits, i32x4* partial, hipStream_t st) {
+  int i = 0;
+#define MDZ_I8_TILE_LAUNCH(WR, WC, MT, NT, NS, STAGE, ALL) \
+  if (tile == i++) return launch_tile<WR, WC, MT, NT, NS, TO, PARTIAL>(p, splits, partial, st);
+  MDZ_I8_TILES(MDZ_I8_TILE_LAUNCH)
+  MDZ_FAIL(MDZ_EINVAL, "linear_i8: no tile %d", tile);
+}
+
+int launch_i8_tile(int out_dtype, const I8Product& p, int tile, int splits, void* partial, hipStream_t st) {
+  if (splits == 1) MDZ_WITH_ELEM(out_dtype, return (launch_by_tile<E, false>(p, tile, 1, nullptr, st)));
+  int rc = launch_by_tile<float, true>(p, tile, splits, (i32x4*)partial, st);
+  if (rc) return rc;
+  const int64_t quads = (int64_t)p.M * p.n_tiles * 4;
+  MDZ_WITH_ELEM(out_dtype, (launch_timed(PROF_GEMM_I8, gemm_i8_finish_kernel<E>, (unsigned)((quads + 255) / 256), 256, 0, st, p,
+                                         (const i32x4*)partial, splits)));
+  MDZ_LAUNCH_CHECK();
+  return MDZ_OK;
+}
+
+}  // namespace mdz

@@ -92,6 +92,7 @@ def test_refusals_are_status_codes():
         lib.medusa_linear_i8(A, A, A + 4, 1, 16, 64, B, A, None, 0, None),
         lib.medusa_linear_i8(A, A, A, 1, 16, 64, B, A + 1, None, 0, None),
         lib.medusa_linear_i8(A, A + 2, A, 1, 16, 64, B, A, None, 0, None),
+        lib.medusa_linear_i8(A, A, A, 64, 16, 64, B, A, A + 4, 1 << 40, None),
         lib.medusa_linear_i8(A, A, A, -1, 16, 64, B, A, None, 0, None),
     ]
     assert rows == [-1] * len(rows)
@@ -101,6 +102,9 @@ def test_refusals_are_status_codes():
     assert lib.medusa_pack_weight_i8(B, A, 16, 131072, A, 16, 0, None) == -3
     assert lib.medusa_linear_i8(A, A, A, 1, 16, 131072, B, A, None, 0, None) == -3
     assert b"131071" in lib.medusa_last_error()
+    need = P.medusa_linear_i8_workspace_bytes(64, 16, 64)
+    assert lib.medusa_linear_i8(A, A, A, 64, 16, 64, B, A, A, need - 1, None) == -4
+    assert lib.medusa_linear_i8(A, A, A, 64, 16, 64, B, A, None, need, None) == -4
     # no rows: nothing to do, and nothing is read
     assert lib.medusa_quantize_rows_i8(B, None, 0, 8, None, None, None, None) == 0
     assert lib.medusa_swiglu_i8(B, None, 0, 8, None, None, None, None) == 0
