@@ -64,6 +64,10 @@ int medusa_gemm_many_rows_plan(int dtype, int M, int N, int K, int max_split, in
 int medusa_attention_plan(const mdz_model_desc* model, int kv_quant, int B, int max_prefix, int fused, int32_t* kernel, int32_t* queries,
                           int32_t* splits, int32_t* ordered);
 
+/* How medusa_linear_i8 cuts a product of M rows: the tile of a workgroup and into how many parts K is split.  Up to 16 rows (32 where neither
+ * rows nor weights are long) weights go straight to registers: tile_rows is then 16 or 32 and tile_cols 16, 32 or 48.  Needs no device. */
+int medusa_linear_i8_plan(int M, int N, int K, int32_t* tile_rows, int32_t* tile_cols, int32_t* k_splits);
+
 /* ---- test hook --------------------------------------------------------------------------------------- */
 
 /* The layer runs RoPE + cache write either fused into the attention kernel's prologue (default) or as a kernel of

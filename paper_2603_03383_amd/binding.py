@@ -85,6 +85,7 @@ _SIGNATURES = {
     "medusa_residual_rmsnorm_i8": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_float, C.c_int, C.c_int] + [C.c_void_p] * 5),
     "medusa_swiglu_i8": (C.c_int, [C.c_int, C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 4),
     "medusa_linear_i8_workspace_bytes": (C.c_int64, [C.c_int] * 3),
+    "medusa_linear_i8_plan": (C.c_int, [C.c_int] * 3 + [C.c_void_p] * 3),
     "medusa_linear_i8": (C.c_int, [C.c_void_p] * 3 + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "medusa_kv_bytes": (C.c_int64, [C.POINTER(KvDesc)]),
     "medusa_kv_init": (C.c_int, [C.POINTER(KvDesc), C.c_void_p]),
@@ -142,7 +143,9 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream(stream) -> C.c_void_p:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # (the handle itself where torch has a call for it: a Stream object takes 3 us to make)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        stream = torch.cuda.current_stream() if raw is None else raw(torch.cuda.current_device())
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -249,23 +252,32 @@ MDZ_I8_TILE_ROWS = 16
 _STORAGE = {torch.bfloat16: MDZ_BF16, torch.float16: MDZ_FP16, torch.float32: MDZ_FP32}
 
 
-def _operand(name: str, t: Optional[torch.Tensor], shape, dtype) -> Optional[int]:
-    """Address of a tensor that has this shape and type; None stays None."""
+def _operand(name: str, t: Optional[torch.Tensor], shape, dtype, device: int) -> Optional[int]:
+    """Address of a tensor that has this shape and type and lies on this GPU; None stays None."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape:
         raise MedusaError(-2, f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
     if not t.is_contiguous():
         raise MedusaError(-2, f"{name}: tensors handed to the library must be contiguous")
+    if device < 0 or t.get_device() != device:
+        raise MedusaError(-1, f"{name}: on {t.device}; a call's tensors lie on one GPU")
     return t.data_ptr()
 
 
+def _stream_of(device: int, stream) -> C.c_void_p:
+    """The caller's stream, or the current one, for tensors on this GPU: the library launches on the current device."""
+    if torch.cuda.current_device() != device:
+        raise MedusaError(-1, f"the tensors lie on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream(stream)
+
+
 def _rows(name: str, t: torch.Tensor):
-    """(shape, storage dtype) of a tensor of rows."""
+    """(shape, storage dtype, GPU) of a tensor of rows."""
     shape, dtype = t.shape, _STORAGE.get(t.dtype)
     if len(shape) != 2 or dtype is None:
         raise MedusaError(-2, f"{name}: {tuple(shape)} {t.dtype}, expected rows of a storage dtype")
-    return shape, dtype
+    return shape, dtype, t.get_device()
 
 
 @functools.lru_cache(maxsize=None)
@@ -273,74 +285,83 @@ def medusa_packed_i8_bytes(n_rows: int, k: int) -> int:
     return _check(lib().medusa_packed_i8_bytes(n_rows, k))
 
 
-def _packed_i8(dst: torch.Tensor, dst_rows: int, k: int) -> int:
+def _packed_i8(dst: torch.Tensor, dst_rows: int, k: int, device: int) -> int:
     if dst.numel() * dst.element_size() < medusa_packed_i8_bytes(dst_rows, k):
         raise MedusaError(-2, f"packed: {dst.numel() * dst.element_size()} bytes are too few for [{dst_rows}, {k}]")
-    return _operand("packed", dst, dst.shape, dst.dtype)
+    return _operand("packed", dst, dst.shape, dst.dtype, device)
 
 
 def medusa_pack_weight_i8(src: torch.Tensor, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0, stream=None) -> None:
     """src [n, k] of a storage dtype -> rows 16 * tile_offset .. of the packed 8-bit matrix dst, quantised per row."""
-    shape, dtype = _rows("src", src)
-    _check(lib().medusa_pack_weight_i8(dtype, _operand("src", src, shape, src.dtype), shape[0], shape[1],
-                                       _packed_i8(dst, dst_rows, shape[1]), dst_rows, tile_offset, _stream(stream)))
+    shape, dtype, gpu = _rows("src", src)
+    _check(lib().medusa_pack_weight_i8(dtype, _operand("src", src, shape, src.dtype, gpu), shape[0], shape[1],
+                                       _packed_i8(dst, dst_rows, shape[1], gpu), dst_rows, tile_offset, _stream_of(gpu, stream)))
 
 
 def medusa_pack_codes_i8(codes: torch.Tensor, scales: torch.Tensor, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0,
                          stream=None) -> None:
     """codes int8 [n, k] with scales fp32 [n] -> the same rows of the packed 8-bit matrix dst."""
     n, k = codes.shape
-    _check(lib().medusa_pack_codes_i8(_operand("codes", codes, (n, k), torch.int8), _operand("scales", scales, (n,), torch.float32), n, k,
-                                      _packed_i8(dst, dst_rows, k), dst_rows, tile_offset, _stream(stream)))
+    gpu = codes.get_device()
+    _check(lib().medusa_pack_codes_i8(_operand("codes", codes, (n, k), torch.int8, gpu), _operand("scales", scales, (n,), torch.float32, gpu),
+                                      n, k, _packed_i8(dst, dst_rows, k, gpu), dst_rows, tile_offset, _stream_of(gpu, stream)))
 
 
 def medusa_quantize_rows_i8(src, codes, scales, values=None, stream=None) -> None:
     """src [rows, d] -> codes int8 [rows, d], scales fp32 [rows]; values (optional, src's type): what they stand for."""
-    shape, dtype = _rows("src", src)
+    shape, dtype, gpu = _rows("src", src)
     rows, d = shape
-    _check(lib().medusa_quantize_rows_i8(dtype, _operand("src", src, shape, src.dtype), rows, d, _operand("codes", codes, shape, torch.int8),
-                                         _operand("scales", scales, (rows,), torch.float32), _operand("values", values, shape, src.dtype),
-                                         _stream(stream)))
+    _check(lib().medusa_quantize_rows_i8(
+        dtype, _operand("src", src, shape, src.dtype, gpu), rows, d, _operand("codes", codes, shape, torch.int8, gpu),
+        _operand("scales", scales, (rows,), torch.float32, gpu), _operand("values", values, shape, src.dtype, gpu), _stream_of(gpu, stream)))
 
 
 def medusa_residual_rmsnorm_i8(x, delta, gain, eps: float, x_out, codes, scales, values=None, stream=None) -> None:
     """x [rows, d] fp32 (+ delta, fp32 or gain's type, or None) -> x_out (x itself, another, or None) and RMSNorm(x') in 8 bits."""
-    shape, _ = _rows("x", x)
+    shape, _, gpu = _rows("x", x)
     rows, d = shape
     td, td_delta = gain.dtype, torch.float32 if delta is None or delta.dtype is torch.float32 else gain.dtype
     if td not in _STORAGE:
         raise MedusaError(-2, f"gain: {td} is no storage dtype")
     _check(lib().medusa_residual_rmsnorm_i8(
-        _STORAGE[td], _operand("x", x, shape, torch.float32), _operand("delta", delta, shape, td_delta), _STORAGE[td_delta],
-        _operand("gain", gain, (d,), td), eps, rows, d, _operand("x_out", x_out, shape, torch.float32),
-        _operand("codes", codes, shape, torch.int8), _operand("scales", scales, (rows,), torch.float32),
-        _operand("values", values, shape, td), _stream(stream)))
+        _STORAGE[td], _operand("x", x, shape, torch.float32, gpu), _operand("delta", delta, shape, td_delta, gpu), _STORAGE[td_delta],
+        _operand("gain", gain, (d,), td, gpu), eps, rows, d, _operand("x_out", x_out, shape, torch.float32, gpu),
+        _operand("codes", codes, shape, torch.int8, gpu), _operand("scales", scales, (rows,), torch.float32, gpu),
+        _operand("values", values, shape, td, gpu), _stream_of(gpu, stream)))
 
 
 def medusa_swiglu_i8(gate_up, codes, scales, values=None, stream=None) -> None:
     """gate_up [rows, 2 ffn] (gate | up) -> SiLU(gate) * up in 8 bits, codes [rows, ffn]."""
-    (rows, width), dtype = _rows("gate_up", gate_up)
+    (rows, width), dtype, gpu = _rows("gate_up", gate_up)
     shape = (rows, width // 2)
-    _check(lib().medusa_swiglu_i8(dtype, _operand("gate_up", gate_up, (rows, shape[1] * 2), gate_up.dtype), rows, shape[1],
-                                  _operand("codes", codes, shape, torch.int8), _operand("scales", scales, (rows,), torch.float32),
-                                  _operand("values", values, shape, gate_up.dtype), _stream(stream)))
+    _check(lib().medusa_swiglu_i8(
+        dtype, _operand("gate_up", gate_up, (rows, shape[1] * 2), gate_up.dtype, gpu), rows, shape[1],
+        _operand("codes", codes, shape, torch.int8, gpu), _operand("scales", scales, (rows,), torch.float32, gpu),
+        _operand("values", values, shape, gate_up.dtype, gpu), _stream_of(gpu, stream)))
 
 
 def medusa_linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
     return _check(lib().medusa_linear_i8_workspace_bytes(M, N, K))
 
 
+def medusa_linear_i8_plan(M: int, N: int, K: int) -> dict:
+    vals = [C.c_int32() for _ in range(3)]
+    _check(lib().medusa_linear_i8_plan(M, N, K, *[C.byref(v) for v in vals]))
+    return dict(zip(("tile_rows", "tile_cols", "k_splits"), [v.value for v in vals]))
+
+
 def medusa_linear_i8(codes, scales, packed, y, ws=None, stream=None) -> None:
     """y [M, N] (any storage dtype) = rows (codes [M, K], scales [M]) x the packed 8-bit matrix [N, K], transposed."""
-    shape, out = _rows("y", y)
+    shape, out, gpu = _rows("y", y)
     M, N = shape
     if codes.dim() != 2:
         raise MedusaError(-2, f"codes: {tuple(codes.shape)}, expected rows")
     K = codes.shape[1]
-    _check(lib().medusa_linear_i8(_operand("codes", codes, (M, K), torch.int8), _operand("scales", scales, (M,), torch.float32),
-                                  _packed_i8(packed, N, K), M, N, K, out, _operand("y", y, shape, y.dtype),
-                                  None if ws is None else _operand("ws", ws, ws.shape, ws.dtype),
-                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+    _check(lib().medusa_linear_i8(
+        _operand("codes", codes, (M, K), torch.int8, gpu), _operand("scales", scales, (M,), torch.float32, gpu),
+        _packed_i8(packed, N, K, gpu), M, N, K, out, _operand("y", y, shape, y.dtype, gpu),
+        None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu), 0 if ws is None else ws.numel() * ws.element_size(),
+        _stream_of(gpu, stream)))
 
 
 def medusa_kv_bytes(kv: KvDesc) -> int:

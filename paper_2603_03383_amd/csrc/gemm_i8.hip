@@ -106,15 +106,15 @@ struct I8Plan {
 
 // Up to 16 rows take the kernel above; up to 32 do where neither the rows (K) nor the weights are long, because it loads a row in pieces of
 // 64 bytes, a third slower than the tiles' 128 (us, this kernel / tiles: 24 rows 4096 x 4096 7.0 / 8.9, 32 rows 12288 x 4096 13.1 / 14.2;
-// 22016 x 4096 22.8 / 21.1, 4096 x 11008 16.3 / 14.1).  Beyond, the tile and the number of splits of the least modelled time: a launch, and
-// the longest of what a CU needs for its workgroups, what the chip needs for all, and W from HBM; a split adds a launch and its sums'
-// way to memory and back.  Fitted to 2300 timings (1 .. 2048 rows, 688 x 256 .. 22016 x 4096 and 5120 x 13824): what it picks takes 1.3 %
-// longer than the best of them on average, 13 % at most from 64 rows of 1 MB of weights on.
+// 22016 x 4096 22.8 / 21.1, 4096 x 11008 16.3 / 14.1).  Beyond, the tile and the number of splits of the least modelled time: the longest
+// of what a CU needs for its workgroups, what the chip needs for all, and W from HBM, which idle CUs slow down; a split adds a launch and
+// its sums' way to memory and back.  Fitted to 2300 timings (1 .. 2048 rows, 688 x 256 .. 22016 x 4096 and 5120 x 13824): what it picks
+// takes 0.8 % longer than the best of them on average, and 13 % at most where a launch takes more than 5 us.
 static I8Plan plan_i8(int M, int N, int K) {
   I8Plan best{-1, 1, 0, 0};
   if (M <= 16 || (M <= 32 && K <= 8192 && (int64_t)N * K <= 1 << 26)) return best;
   const int n_pad = (int)i8_padded_rows(N), stages = (K + 127) / 128, cus = num_cus();
-  const float hbm = (float)N * K * (1e-6f / 4.9f);
+  const float hbm = (float)N * K * (1e-6f / 5.4f);
   float least = 0.f;
   for (int t = 0; t < kNumI8Tiles; ++t) {
     const I8Tile& tile = kI8Tiles[t];
@@ -124,9 +124,9 @@ static I8Plan plan_i8(int M, int N, int K) {
       if (splits > 1 && (splits * 4 > stages || blocks * splits > 4 * cus)) break;
       const int64_t wgs = blocks * splits;
       const float s = (float)((stages + splits - 1) / splits);
-      float rounds = (float)((wgs + cus - 1) / cus);
-      if (rounds > 1.f && tile.two) rounds *= 0.86f;
-      float us = fmaxf(fmaxf(rounds * s * tile.us_stage, (float)wgs * s * tile.us_all), hbm);
+      const float rounds = (float)((wgs + cus - 1) / cus);
+      const float cu = rounds * s * tile.us_stage * (rounds > 1.f && tile.two ? 0.81f : 1.f);
+      float us = fmaxf(fmaxf(cu, (float)wgs * s * tile.us_all), hbm * sqrtf(rounds * cus / wgs)) + 0.36f * (rounds - 1.f);
       if (splits > 1) us += 2.f + (float)splits * M * n_pad * (4e-6f / 2.5f);
       if (best.tile < 0 || us < least) best.tile = t, best.splits = splits, least = us;
     }
@@ -136,14 +136,16 @@ static I8Plan plan_i8(int M, int N, int K) {
   return best;
 }
 
+// One 16-column tile per workgroup until every CU has one, then two, then three, whose loads share the rows' (us at 1 row, one / two / three
+// tiles: 4096 x 4096 4.9 / 5.9 / 7.0; 16 rows 6144 x 4096 9.1 / 7.3 / 8.4; 22016 x 4096 17.5 / 17.4 / 16.6)
+static int few_rows_tiles(int n_tiles) { return n_tiles <= num_cus() ? 1 : n_tiles <= 2 * num_cus() ? 2 : 3; }
 template <int MT, typename TO>
 static int launch_few_rows(const I8Product& p, hipStream_t st) {
-  // one 16-column tile per workgroup until every CU has one, then two, then three, whose loads share the rows' (us at 1 row, one / two / three
-  // tiles: 4096 x 4096 4.9 / 5.9 / 7.0; 6144 x 4096, 16 rows 9.1 / 7.3 / 8.4; 22016 x 4096 17.5 / 17.4 / 16.6)
-  const int cus = num_cus();
-  if (p.n_tiles <= cus) return launch_narrow<MT, 1, 4, 4, TO>(p, st);
-  if (p.n_tiles <= 2 * cus) return launch_narrow<MT, 2, 4, 4, TO>(p, st);
-  return launch_narrow<MT, 3, 4, MT == 1 ? 6 : 4, TO>(p, st);
+  switch (few_rows_tiles(p.n_tiles)) {
+    case 1: return launch_narrow<MT, 1, 4, 4, TO>(p, st);
+    case 2: return launch_narrow<MT, 2, 4, 4, TO>(p, st);
+    default: return launch_narrow<MT, 3, 4, MT == 1 ? 6 : 4, TO>(p, st);
+  }
 }
 
 static int check_linear_i8(int M, int N, int K) {
@@ -163,6 +165,16 @@ extern "C" {
 int64_t medusa_linear_i8_workspace_bytes(int M, int N, int K) {
   const int rc = check_linear_i8(M, N, K);
   return rc ? rc : plan_i8(M, N, K).bytes;
+}
+
+int medusa_linear_i8_plan(int M, int N, int K, int32_t* tile_rows, int32_t* tile_cols, int32_t* k_splits) {
+  const int rc = check_linear_i8(M, N, K);
+  if (rc) return rc;
+  const I8Plan p = plan_i8(M, N, K);
+  if (tile_rows) *tile_rows = p.tile >= 0 ? kI8Tiles[p.tile].rows : M <= 16 ? 16 : 32;
+  if (tile_cols) *tile_cols = p.tile >= 0 ? kI8Tiles[p.tile].cols : 16 * few_rows_tiles((int)(i8_padded_rows(N) / kI8TileRows));
+  if (k_splits) *k_splits = p.splits;
+  return MDZ_OK;
 }
 
 int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, int out_dtype, void* y, void* ws,

@@ -150,15 +150,15 @@ static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream
 // rings of small stages (a CU's intake is the bound, and two workgroups per CU cover each other's start and end); many rows take the
 // largest tiles, which need the fewest bytes per product.
 #define MDZ_I8_TILES(T)         \
-  T(2, 2, 1, 1, 8, .168, .385)  \
-  T(4, 1, 1, 3, 5, .247, 1.02)  \
-  T(2, 2, 2, 2, 4, .302, 1.03)  \
-  T(4, 3, 1, 2, 4, .364, 1.60)  \
-  T(2, 4, 3, 1, 5, .371, 1.45)  \
-  T(2, 4, 4, 1, 4, .417, 1.73)  \
-  T(2, 4, 4, 2, 4, .624, 2.55)  \
-  T(4, 4, 4, 2, 3, .947, 3.92)  \
-  T(4, 2, 4, 6, 2, 1.307, 6.06)
+  T(2, 2, 1, 1, 8, .169, .405)  \
+  T(4, 1, 1, 3, 5, .244, .985)  \
+  T(2, 2, 2, 2, 4, .306, .997)  \
+  T(4, 3, 1, 2, 4, .354, 1.58)  \
+  T(2, 4, 3, 1, 5, .369, 1.44)  \
+  T(2, 4, 4, 1, 4, .415, 1.73)  \
+  T(2, 4, 4, 2, 4, .618, 2.54)  \
+  T(4, 4, 4, 2, 3, .948, 3.93)  \
+  T(4, 2, 4, 6, 2, 1.310, 6.08)
 #define MDZ_I8_TILE_FACTS(WR, WC, MT, NT, NS, STAGE, ALL) \
   {WR * MT * 16, WC * NT * 16, (WR * MT + WC * NT) * 2048 * NS <= 80 * 1024, STAGE##f, ALL##f * 1e-3f},
 const I8Tile kI8Tiles[kNumI8Tiles] = {MDZ_I8_TILES(MDZ_I8_TILE_FACTS)};

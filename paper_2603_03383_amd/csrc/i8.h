@@ -13,15 +13,31 @@ constexpr float kI8Max = 127.f;
 // max|t| is kept as its bits: as integers, the magnitudes of fp32 numbers order as the numbers do, then infinity, then NaN
 __device__ inline uint32_t abs_bits(float t) { return __float_as_uint(t) & 0x7FFFFFFFu; }
 struct I8Quantiser {
-  float scale;
-  bool bad;
+  float scale, inverse;
+  bool bad, plain;  // plain: the quotient below is good; else the division is left to the compiler's sequence for it
   __device__ explicit I8Quantiser(uint32_t amax_bits) {
     bad = amax_bits >= 0x7F800000u;
     const float s = __uint_as_float(amax_bits) / kI8Max;
     scale = bad ? __uint_as_float(0x7FC00000u) : s > 0.f ? s : 1.f;
+    inverse = 1.f / scale;
+    plain = scale >= 0x1p-100f && scale <= 0x1p100f;
   }
-  __device__ inline float round(float t) const {  // the code, as a number
-    return bad ? 0.f : fminf(fmaxf(rintf(t / scale), -kI8Max), kI8Max);
+  __device__ inline float code(float quotient) const { return __builtin_amdgcn_fmed3f(rintf(quotient), -kI8Max, kI8Max); }
+  // The codes of W values, as numbers.  Three operations make the rounded quotient: a product with the rounded reciprocal, the rest it
+  // leaves, which is exact, and the rest's share (1024 rows of 12800 with SwiGLU: 25.2 us with the
+  // compiler's divisions, 21.8 so; 4000 plain rows of 1387: 11.4 / 9.2).
+  template <int W>
+  __device__ inline void round(const float (&t)[W], float (&c)[W]) const {
+    if (plain) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) {
+        const float q = t[e] * inverse;
+        c[e] = code(fmaf(fmaf(-q, scale, t[e]), inverse, q));
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e) c[e] = bad ? 0.f : code(t[e] / scale);
+    }
   }
 };
 

@@ -1,83 +1,292 @@
 // Rows in 8 bits with one scale each: the residual's addition and RMSNorm, SwiGLU, plain rows, and the packing of 8-bit weights.
+//
+// A row is one workgroup's: its elements are read once, stay in registers while max|t| (and the norm's sum of squares) go around the
+// workgroup in a single exchange, and leave as codes.  The norm needs no second exchange for its factor, because 1 / rms is positive:
+// the codes of x' * gain / rms are those of x' * gain, and the factor goes into the scale.  So the codes do not depend on the order of any sum.
+// What bounds it: up to a row per CU the latency of one load, one exchange and one store (about 4 us as a launch, 64 rows of 4096 like
+// one); beyond, memory: norm 1024 x 5120 (16-bit update, 16-bit values written too) 14.2 us = 4.8 TB/s, 4096 x 8192 78 us = 5.6 TB/s, SwiGLU
+// 1024 x 12800 20.7 us = 4.4 TB/s, 2048 x 11008 33 us = 4.7 TB/s, against 4.9 TB/s of a large copy.
 #include "i8.h"
 
 namespace mdz {
 
-template <typename T>
-__device__ inline T block_reduce_256(T v, T* smem4, T (*op)(T, T)) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
-  if ((threadIdx.x & 63) == 0) smem4[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return op(op(smem4[0], smem4[1]), op(smem4[2], smem4[3]));
-}
-__device__ inline float add_f(float a, float b) { return a + b; }
 __device__ inline uint32_t max_u(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// Where a kernel's rows come from: element i of row r as fp32, read once for the statistics and once for the codes.
+// Over a wave by lane permutations (no trip through LDS), the result in every lane: rows of 16 lanes first, then across them.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <typename Op>
+__device__ inline uint32_t wave_reduce(uint32_t v, Op op) {  // zero bits are neutral
+  v = op(v, dpp<0x111, 0xf>(v));  // row_shr 1, 2, 4, 8: lane 15 of a row has the row
+  v = op(v, dpp<0x112, 0xf>(v));
+  v = op(v, dpp<0x114, 0xf>(v));
+  v = op(v, dpp<0x118, 0xf>(v));
+  v = op(v, dpp<0x142, 0xa>(v));  // lane 15 of a row to the next row (1 and 3), lane 31 to the rows 2 and 3
+  v = op(v, dpp<0x143, 0xc>(v));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ inline float wave_sum(float v) {
+  return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ inline uint32_t wave_max(uint32_t v) { return wave_reduce(v, max_u); }
+
+// A row's statistics over the workgroup: max|t| (bits) and the sum of squares, in one exchange.
+__device__ inline void row_statistics(uint32_t& amax, float& squares) {
+  __shared__ uint32_t wave_amax[16];
+  __shared__ float wave_squares[16];
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  amax = wave_max(amax), squares = wave_sum(squares);
+  if ((threadIdx.x & 63) == 0) wave_amax[wave] = amax, wave_squares[wave] = squares;
+  __syncthreads();
+  amax = 0, squares = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    const uint32_t a = wave_amax[w];
+    const float q = wave_squares[w];
+    amax = w < waves ? max_u(amax, a) : amax, squares += w < waves ? q : 0.f;
+  }
+}
+
+// W elements as one load or store of any alignment
+template <int BYTES>
+struct Piece;
+template <>
+struct Piece<4> {
+  typedef uint32_t Bits;
+  typedef Bits Any __attribute__((aligned(1)));
+};
+template <>
+struct Piece<8> {
+  typedef uint32_t Bits __attribute__((ext_vector_type(2)));
+  typedef Bits Any __attribute__((aligned(1)));
+};
+template <>
+struct Piece<16> {
+  typedef u32x4_t Bits;
+  typedef Bits Any __attribute__((aligned(1)));
+};
+template <typename E, int W>
+struct Elems {
+  E v[W];
+};
+// W consecutive elements of a row.  TAIL (the row's width is no multiple of W): near its end `n` < W are there, the others come as zero.
+template <bool TAIL, int W, typename E>
+__device__ inline Elems<E, W> fetch(const E* src, int n) {
+  typedef Piece<W * sizeof(E)> P;
+  typedef Elems<E, W> Some;
+  Some s;
+  if (!TAIL || n >= W) {
+    const typename P::Bits bits = *reinterpret_cast<const typename P::Any*>(src);
+    s = __builtin_bit_cast(Some, bits);
+  } else {
+#pragma unroll
+    for (int e = 0; e < W; ++e) s.v[e] = e < n ? src[e] : E{};
+  }
+  return s;
+}
+template <bool TAIL, int W, typename E>
+__device__ inline void put(E* dst, int n, const Elems<E, W>& s) {
+  typedef Piece<W * sizeof(E)> P;
+  if (!TAIL || n >= W) {
+    *reinterpret_cast<typename P::Any*>(dst) = __builtin_bit_cast(typename P::Bits, s);
+  } else {
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+      if (e < n) dst[e] = s.v[e];
+  }
+}
+
+// Where a kernel's rows come from: `load` requests kW elements of row r from element i on, `n` of them inside the row, and `values` makes
+// them numbers.
 template <typename E>
 struct PlainRows {
+  static constexpr int kW = 16 / sizeof(E);
+  struct Raw {
+    Elems<E, kW> x;
+  };
   const E* src;
   int d;
-  __device__ inline float first(int64_t r, int i, float&) const { return to_float(src[r * d + i]); }
-  __device__ inline float again(int64_t r, int i) const { return to_float(src[r * d + i]); }
-  __device__ inline float factor(float) const { return 1.f; }
-};
-template <typename E>
-struct SwigluRows {
-  const E* gate_up;
-  int d;
-  __device__ inline float first(int64_t r, int i, float&) const { return again(r, i); }
-  __device__ inline float again(int64_t r, int i) const {
-    const float g = to_float(gate_up[r * 2 * d + i]), u = to_float(gate_up[r * 2 * d + d + i]);
-    return g / (1.f + expf(-g)) * u;
+  template <bool TAIL>
+  __device__ inline void load(int64_t r, int i, int n, Raw& raw) const {
+    raw.x = fetch<TAIL, kW>(src + r * d + i, n);
+  }
+  template <bool TAIL>
+  __device__ inline void values(int64_t, int, int, const Raw& raw, float (&t)[kW], float&) const {
+#pragma unroll
+    for (int e = 0; e < kW; ++e) t[e] = to_float(raw.x.v[e]);
   }
   __device__ inline float factor(float) const { return 1.f; }
+  __device__ inline void second_reading() {}
+};
+// 1 / (1 + e^-g): the exponential's argument in two parts, so that its rounding does not grow with g; one unit in the last place each for
+// the exponential and the reciprocal
+__device__ inline float sigmoid_i8(float g) {
+  constexpr float kLog2e = 1.44269504f, kLow = 1.92596303e-8f;  // log2(e) = their sum
+  const float hi = -g * kLog2e;
+  const float lo = fmaf(-g, kLog2e, -hi) - g * kLow;
+  const float e = fast_exp2(hi);
+  // (beyond 2^100 the sigmoid is e^g to the last bit, and far beyond e is infinite, where the correction would make a NaN of it)
+  return __builtin_amdgcn_rcpf(1.f + (hi > 100.f ? e : fmaf(e, lo * 0.693147181f, e)));
+}
+template <typename E>
+struct SwigluRows {
+  static constexpr int kW = 16 / sizeof(E);
+  struct Raw {
+    Elems<E, kW> gate, up;
+  };
+  const E* gate_up;
+  int d;
+  template <bool TAIL>
+  __device__ inline void load(int64_t r, int i, int n, Raw& raw) const {
+    raw.gate = fetch<TAIL, kW>(gate_up + r * 2 * d + i, n);
+    raw.up = fetch<TAIL, kW>(gate_up + r * 2 * d + d + i, n);
+  }
+  template <bool TAIL>
+  __device__ inline void values(int64_t, int, int, const Raw& raw, float (&t)[kW], float&) const {
+#pragma unroll
+    for (int e = 0; e < kW; ++e) {
+      const float g = to_float(raw.gate.v[e]);
+      t[e] = g * sigmoid_i8(g) * to_float(raw.up.v[e]);
+    }
+  }
+  __device__ inline float factor(float) const { return 1.f; }
+  __device__ inline void second_reading() {}
 };
 // x' = x + delta; the codes are those of x' * gain, because the norm's factor is positive and cancels; it goes into the scale
 template <typename E, typename D>
 struct NormRows {
+  static constexpr int kW = 4;
+  struct Raw {
+    Elems<float, kW> x;
+    Elems<D, kW> delta;
+    Elems<E, kW> gain;
+  };
   const float* x;
   const D* delta;
   const E* gain;
   float* x_out;
   int d;
   float eps;
-  __device__ inline float sum(int64_t r, int i) const { return delta ? x[r * d + i] + to_float(delta[r * d + i]) : x[r * d + i]; }
-  __device__ inline float first(int64_t r, int i, float& squares) const {
-    const float v = sum(r, i);
-    if (x_out) x_out[r * d + i] = v;  // (x_out may be x: the second reading is of x_out)
-    squares += v * v;
-    return v * to_float(gain[i]);
+  template <bool TAIL>
+  __device__ inline void load(int64_t r, int i, int n, Raw& raw) const {
+    raw.x = fetch<TAIL, kW>(x + r * d + i, n);
+    if (delta) raw.delta = fetch<TAIL, kW>(delta + r * d + i, n);
+    raw.gain = fetch<TAIL, kW>(gain + i, n);
   }
-  __device__ inline float again(int64_t r, int i) const { return (x_out ? x_out[r * d + i] : sum(r, i)) * to_float(gain[i]); }
+  template <bool TAIL>
+  __device__ inline void values(int64_t r, int i, int n, const Raw& raw, float (&t)[kW], float& squares) const {
+    Elems<float, kW> sum = raw.x;
+    if (delta) {
+#pragma unroll
+      for (int e = 0; e < kW; ++e) sum.v[e] += to_float(raw.delta.v[e]);
+    }
+    if (x_out && n > 0) put<TAIL, kW>(x_out + r * d + i, n, sum);
+#pragma unroll
+    for (int e = 0; e < kW; ++e) {
+      squares += n > 0 ? sum.v[e] * sum.v[e] : 0.f;
+      t[e] = sum.v[e] * to_float(raw.gain.v[e]);
+    }
+  }
   __device__ inline float factor(float squares) const { return 1.f / sqrtf(squares / (float)d + eps); }
+  // a thread reads again what it wrote itself: x_out may be x, which holds the sum by then
+  __device__ inline void second_reading() {
+    if (x_out) x = x_out, delta = nullptr, x_out = nullptr;
+  }
 };
 
-template <typename Rows, typename E>
-__global__ void __launch_bounds__(256) rows_i8_kernel(Rows in, int d, int8_t* codes, float* scales, E* values) {
-  __shared__ float red_f[4];
-  __shared__ uint32_t red_u[4];
+// codes of t and what they stand for, W at a time
+template <bool TAIL, typename E, int W>
+__device__ inline void put_codes(const I8Quantiser& q, const float (&t)[W], int n, float scale, int8_t* codes, E* values) {
+  Elems<int8_t, W> c;
+  Elems<E, W> v;
+  float code[W];
+  q.round(t, code);
+#pragma unroll
+  for (int e = 0; e < W; ++e) {
+    c.v[e] = (int8_t)(int)code[e];
+    v.v[e] = from_float<E>(code[e] * scale);
+  }
+  put<TAIL, W>(codes, n, c);
+  if (values) put<TAIL, W>(values, n, v);
+}
+
+// One workgroup per row, whose elements stay in registers from the statistics to the codes: a thread has NV pieces of kW.
+template <typename Rows, typename E, int NV, bool TAIL>
+__global__ void __launch_bounds__(1024) rows_i8_kernel(Rows in, int d, int8_t* codes, float* scales, E* values) {
+  constexpr int W = Rows::kW;
   const int64_t r = blockIdx.x;
-  float squares = 0.f;
+  typename Rows::Raw raw[NV];
+  float t[NV][W], squares = 0.f;
   uint32_t amax = 0;
-  for (int i = threadIdx.x; i < d; i += 256) amax = max_u(amax, abs_bits(in.first(r, i, squares)));
-  amax = block_reduce_256(amax, red_u, max_u);
-  squares = block_reduce_256(squares, red_f, add_f);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {  // everything is requested before the first of it is used; beyond the row its start again
+    const int i = (threadIdx.x + k * blockDim.x) * W;
+    in.template load<TAIL>(r, i < d ? i : 0, TAIL ? d - i : W, raw[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = (threadIdx.x + k * blockDim.x) * W;
+    in.template values<TAIL>(r, i, d - i, raw[k], t[k], squares);
+#pragma unroll
+    for (int e = 0; e < W; ++e) amax = max_u(amax, i < d ? abs_bits(t[k][e]) : 0u);
+  }
+  row_statistics(amax, squares);
   const I8Quantiser q(amax);
   const float scale = q.scale * in.factor(squares);
   if (threadIdx.x == 0) scales[r] = scale;
-  for (int i = threadIdx.x; i < d; i += 256) {
-    const float c = q.round(in.again(r, i));
-    codes[r * d + i] = (int8_t)c;
-    if (values) values[r * d + i] = from_float<E>(c * scale);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = (threadIdx.x + k * blockDim.x) * W;
+    if (i < d) put_codes<TAIL, E, W>(q, t[k], d - i, scale, codes + r * d + i, values ? values + r * d + i : nullptr);
   }
 }
 
+// Rows longer than the registers of a workgroup: read twice.
+template <typename Rows, typename E>
+__global__ void __launch_bounds__(1024) rows_i8_long_kernel(Rows in, int d, int8_t* codes, float* scales, E* values) {
+  constexpr int W = Rows::kW;
+  const int64_t r = blockIdx.x;
+  typename Rows::Raw raw;
+  float t[W], squares = 0.f;
+  uint32_t amax = 0;
+  for (int i = threadIdx.x * W; i < d; i += 1024 * W) {
+    in.template load<true>(r, i, d - i, raw);
+    in.template values<true>(r, i, d - i, raw, t, squares);
+#pragma unroll
+    for (int e = 0; e < W; ++e) amax = max_u(amax, abs_bits(t[e]));
+  }
+  row_statistics(amax, squares);
+  const I8Quantiser q(amax);
+  const float scale = q.scale * in.factor(squares);
+  if (threadIdx.x == 0) scales[r] = scale;
+  in.second_reading();
+  for (int i = threadIdx.x * W; i < d; i += 1024 * W) {
+    float unused = 0.f;
+    in.template load<true>(r, i, d - i, raw);
+    in.template values<true>(r, i, d - i, raw, t, unused);
+    put_codes<true, E, W>(q, t, d - i, scale, codes + r * d + i, values ? values + r * d + i : nullptr);
+  }
+}
+
+template <typename E, bool TAIL, typename Rows>
+static auto rows_i8_variant(const Rows&, int nv) {
+  return nv == 1 ? rows_i8_kernel<Rows, E, 1, TAIL> : nv == 2 ? rows_i8_kernel<Rows, E, 2, TAIL> : rows_i8_kernel<Rows, E, 4, TAIL>;
+}
 template <typename E, typename Rows>
 static int launch_rows_i8(const Rows& in, int rows, int d, int8_t* codes, float* scales, void* values, hipStream_t st) {
   if (rows == 0) return MDZ_OK;
-  launch_timed(PROF_ROWS_I8, rows_i8_kernel<Rows, E>, rows, 256, 0, st, in, d, codes, scales, (E*)values);
+  const int pieces = (d + Rows::kW - 1) / Rows::kW;
+  // Up to a row per CU a row's time is the latency of one thread's chain, so a thread takes as little as it can; with more rows, small
+  // workgroups leave a CU no idle while one of them starts or ends.  us with up to 1024 / 256 threads before a thread takes more:
+  // SwiGLU 64 x 11008 5.0 / 6.0; norm 1024 x 5120 16.2 / 14.2, 1024 x 4096 14.9 / 12.6, SwiGLU 1024 x 12800 22.2 / 20.9.
+  const int most = rows <= num_cus() ? 1024 : 256;
+  const int nv = pieces <= most ? 1 : pieces <= 2 * most ? 2 : 4;
+  int threads = ((pieces + nv - 1) / nv + 63) / 64 * 64;
+  auto kernel = d % Rows::kW ? rows_i8_variant<E, true>(in, nv) : rows_i8_variant<E, false>(in, nv);
+  if (pieces > 4096) kernel = rows_i8_long_kernel<Rows, E>, threads = 1024;
+  launch_timed(PROF_ROWS_I8, kernel, rows, threads, 0, st, in, d, codes, scales, (E*)values);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
 }
@@ -86,16 +295,19 @@ static int launch_rows_i8(const Rows& in, int rows, int d, int8_t* codes, float*
 template <typename E>
 __global__ void __launch_bounds__(256) pack_weight_i8_kernel(const E* src, int64_t n_rows, int64_t k, uint8_t* dst, int64_t kp,
                                                              int64_t first_row, float* scales) {
-  __shared__ uint32_t red[4];
   const int64_t n = blockIdx.x, row = first_row + n;
   uint32_t amax = 0;
+  float unused = 0.f;
   if (n < n_rows)
     for (int64_t i = threadIdx.x; i < k; i += 256) amax = max_u(amax, abs_bits(to_float(src[n * k + i])));
-  amax = block_reduce_256(amax, red, max_u);
+  row_statistics(amax, unused);
   const I8Quantiser q(amax);
   if (threadIdx.x == 0) scales[row] = n < n_rows ? q.scale : 0.f;
-  for (int64_t i = threadIdx.x; i < kp; i += 256)
-    dst[i8_index(row, i, kp)] = (uint8_t)(n < n_rows && i < k ? (int8_t)q.round(to_float(src[n * k + i])) : 0);
+  for (int64_t i = threadIdx.x; i < kp; i += 256) {
+    float t[1] = {n < n_rows && i < k ? to_float(src[n * k + i]) : 0.f}, c[1];
+    q.round(t, c);
+    dst[i8_index(row, i, kp)] = (uint8_t)(int8_t)(int)c[0];
+  }
 }
 
 __global__ void __launch_bounds__(256) pack_codes_i8_kernel(const int8_t* codes, const float* src_scales, int64_t n_rows, int64_t k,

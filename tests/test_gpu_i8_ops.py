@@ -201,6 +201,27 @@ def test_linear(out, m, n, k):
     check_linear(*make_linear(m, n, k), out)
 
 
+# (tile rows, tile columns, parts of K) that a product of (rows, columns) over about so many features is cut into: every tile, whole and in parts
+PLANS = [((16, 16, 1), (1, 50, 1150)), ((16, 32, 1), (9, 4305, 1150)), ((16, 48, 1), (16, 8355, 1150)), ((32, 16, 1), (17, 30, 1150)),
+         ((32, 32, 1), (33, 47, 1146)), ((32, 32, 4), (33, 17, 2645)), ((32, 48, 1), (17, 8327, 1109)), ((64, 48, 1), (34, 4110, 1121)),
+         ((64, 48, 6), (1352, 16, 3659)), ((64, 64, 1), (65, 6478, 1113)), ((64, 64, 8), (1057, 50, 4004)), ((64, 96, 1), (67, 8235, 1131)),
+         ((64, 96, 8), (66, 1113, 4949)), ((96, 64, 1), (65, 11368, 1147)), ((96, 64, 6), (67, 1832, 3756)), ((128, 64, 1), (97, 12831, 1127)),
+         ((128, 64, 6), (99, 2114, 4477)), ((128, 128, 1), (65, 17990, 1112)), ((128, 128, 4), (66, 5473, 6556)),
+         ((256, 128, 1), (131, 18221, 1136)), ((256, 128, 6), (140, 4113, 7383)), ((256, 192, 1), (263, 21915, 1139)),
+         ((256, 192, 4), (129, 11332, 7474))]
+
+
+@pytest.mark.parametrize("plan,shape", PLANS)
+def test_linear_every_tile(plan, shape):
+    """More stages than any ring has, row and column blocks that end inside a tile; features that end inside a cache line, and rows that
+    start anywhere and go through the workspace."""
+    m, n, k = shape
+    for k in (k // 16 * 16 + 16, k | 1):
+        got = P.medusa_linear_i8_plan(m, n, k)
+        assert (got["tile_rows"], got["tile_cols"], got["k_splits"]) == plan
+        check_linear(*make_linear(m, n, k), "bf16")
+
+
 @pytest.mark.parametrize("m,n,k,offset", [(3, 33, 100, 1), (64, 256, 256, 4), (64, 512, 4096, 8), (70, 256, 256, 1), (200, 512, 1024, 3),
                                           (300, 256, 1001, 15)])
 def test_linear_rows_off_alignment(m, n, k, offset):
