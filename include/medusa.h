@@ -70,7 +70,13 @@ typedef enum { MDZ_KV_PLAIN = 0, MDZ_KV_FP8E4M3 = 1 } mdz_kv_quant;
  * terms of a deep bf16 stack's rounding error.  What the layer computes (Section 3.2: the ordinary decoder layer on
  * the tree's rows) is unchanged; every other buffer, the gains, the cache and the other matrices stay bf16.  An
  * activation beyond 65504 in magnitude would overflow: this is an option for models whose feed-forward activations
- * are known to stay inside that range, off by default. */
+ * are known to stay inside that range, off by default.
+ * weights_i8 = 1 (bf16 and fp16 models): the four matrix products of every layer take 8-bit integers (see "8-bit integer
+ * products" below).  The layers' matrices are then packed by medusa_pack_weight_i8 or medusa_pack_codes_i8, one scale per
+ * output feature: half the bytes of the weights.  The products' inputs (both norms' outputs, the attention's output, the
+ * SwiGLU output) are rounded to 8 bits with one scale per row; gate and up are rounded to the storage dtype before the
+ * SwiGLU, everything else is as without it: the residual stream and q, k, v in fp32, the cache, the final norm, the
+ * vocabulary matrices and the Medusa heads in the storage dtype. */
 typedef struct {
   int32_t d, n_heads, head_dim, ffn, vocab, n_layers;
   int32_t dtype; /* mdz_dtype */
@@ -78,13 +84,15 @@ typedef struct {
   float rms_eps;
   float rope_base;
   int32_t n_kv_heads;
-  int32_t ffn_f16; /* 0 or 1; 1 is allowed for MDZ_BF16 only (see below) */
+  int32_t ffn_f16; /* 0 or 1; 1 is allowed for MDZ_BF16 only (see above) */
+  int32_t weights_i8; /* 0 or 1; 1 needs a 16-bit dtype and ffn_f16 = 0 (see above) */
 } mdz_model_desc;
 
 /* HOST struct of device pointers: one decoder layer.  Matrices are in the library's PACKED layout
  * (see medusa_pack_weight): wqkv = rows of Wq, Wk, Wv stacked
  * ([d + 2 * n_kv_heads * head_dim, d]: 3d for multi-head attention); wgateup = Wgate and Wup with
- * their row tiles interleaved (tile 2j = gate tile j, tile 2j+1 = up tile j; [2*ffn, d]).
+ * their row tiles interleaved (tile 2j = gate tile j, tile 2j+1 = up tile j; [2*ffn, d]).  With weights_i8 = 1 they are
+ * packed 8-bit matrices, and wgateup = rows of Wgate and Wup stacked.
  * g_attn, g_ffn: RMSNorm gains [d], storage dtype. */
 typedef struct {
   const void* wqkv;

@@ -40,7 +40,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import kv8
+from . import kv8, rows8
 
 F64 = np.float64
 
@@ -117,6 +117,8 @@ def _layer(x, lw, kc, vc, slots, pos, visible, cfg):
     cfg["n_kv_heads"] (default n_heads) key/value heads: wk, wv are [Hkv*hd, d] (Table 1 of the paper: 32 query
     heads, 8 key/value heads).  cfg["kv_quant"] == "fp8e4m3": the rows are written as 8-bit codes with a scale per
     row (the KV compression the paper's Section 4.2 / 5 point to) and read back dequantised."""
+    if cfg.get("weights_i8"):
+        return _layer_8bit(x, lw, kc, vc, slots, pos, visible, cfg)
     H, hd = cfg["n_heads"], cfg["head_dim"]
     Hkv = cfg.get("n_kv_heads") or H
     assert H % Hkv == 0
@@ -142,6 +144,28 @@ def _layer(x, lw, kc, vc, slots, pos, visible, cfg):
     up = xn @ np.asarray(lw["wup"], dtype=F64).T
     x = x + (silu(gate) * up) @ np.asarray(lw["wdown"], dtype=F64).T
     return x
+
+
+def _layer_8bit(x, lw, kc, vc, slots, pos, visible, cfg):
+    """The same layer with its four products in 8-bit integers: they take what the rows of their inputs and of their
+    weights stand for (oracle/rows8.py), weights with one scale per output feature, inputs with one per row."""
+    H, hd = cfg["n_heads"], cfg["head_dim"]
+    Hkv = cfg.get("n_kv_heads") or H
+    n, store = x.shape[0], (lambda r: kv8.roundtrip_rows(r)) if cfg.get("kv_quant") == "fp8e4m3" else (lambda r: round_to_storage(r, cfg["dtype"]))
+
+    def product(rows, *names):
+        rows = rows8.roundtrip_rows(rows)
+        return [rows @ rows8.roundtrip_rows(lw[name]).T for name in names]
+
+    def heads(a, count):
+        return a.reshape(n, count, hd).transpose(1, 0, 2)
+    q, k, v = product(rmsnorm(x, lw["g_attn"], cfg["rms_eps"]), "wq", "wk", "wv")
+    kc[:, slots, :] = store(rope(heads(k, Hkv), pos, cfg["rope_base"]))
+    vc[:, slots, :] = store(heads(v, Hkv))
+    att = _attend(rope(heads(q, H), pos, cfg["rope_base"]), kc, vc, visible, hd)
+    x = x + product(att.transpose(1, 0, 2).reshape(n, H * hd), "wo")[0]
+    gate, up = product(rmsnorm(x, lw["g_ffn"], cfg["rms_eps"]), "wgate", "wup")
+    return x + product(silu(gate) * up, "wdown")[0]
 
 
 def tree_visibility(tree, S):

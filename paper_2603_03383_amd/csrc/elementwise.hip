@@ -232,6 +232,16 @@ int launch_first_norm_and_rope_table(int dtype, float* x, const void* g, void* x
   return launch_norm_with_rope(dtype, dtype, x, single_slot(nullptr, 0, 0), g, xn, rows, d, eps, rope, st);
 }
 
+int launch_rope_table(int tree, const int32_t* seq_len, int B, int max_prefix, int head_dim, float rope_base, float* cs, int32_t* status,
+                      hipStream_t st) {
+  const int entries = B * host_tree(tree)->T * (head_dim / 2);
+  const RopeJob rope{seq_len, cs, status, tree, B, max_prefix, head_dim / 2, (entries + 255) / 256, log2((double)rope_base)};
+  launch_timed(PROF_ROPE, residual_rmsnorm_kernel<float>, rope.n_blocks, 256, 0, st, (float*)nullptr, single_slot(nullptr, 0, 0),
+               (const float*)nullptr, (float*)nullptr, 0, 0.f, /*rows=*/0, rope);
+  MDZ_LAUNCH_CHECK();
+  return MDZ_OK;
+}
+
 // grid (B*T, query heads), block = head_dim/2 threads... generalised: threads stride over i < half.  The QKV GEMM
 // output has the query heads' columns first, then the key heads', then the value heads'; the first query head of a
 // group also rotates and stores its group's key row and stores its value row.

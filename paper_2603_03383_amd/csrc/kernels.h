@@ -58,6 +58,9 @@ int launch_residual_rmsnorm(int dtype, float* x, const Partials& part, const voi
 int launch_first_norm_and_rope_table(int dtype, float* x, const void* g, void* xn, int rows, int d, float eps, int tree,
                                      const int32_t* seq_len, int B, int max_prefix, int head_dim, float rope_base, float* cs,
                                      int32_t* status, hipStream_t st);
+// that table alone
+int launch_rope_table(int tree, const int32_t* seq_len, int B, int max_prefix, int head_dim, float rope_base, float* cs, int32_t* status,
+                      hipStream_t st);
 // rotates q and k of qkv [B*T][3d] fp32 (given as partials); q -> q_out [B*T][d] storage dtype; k,v -> cache
 // slots S_b + n
 int launch_rope_kvwrite(int dtype, int tree, const Partials& qkv, const float* cs, void* q_out, const KvGeom& g,

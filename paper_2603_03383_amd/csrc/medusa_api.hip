@@ -152,6 +152,7 @@ static int ffn_dtype(const mdz_model_desc& m) { return m.ffn_f16 ? (int)MDZ_FP16
 
 struct Workspace {
   int64_t rope_cs, x, xn, part, q, att, u, logits, h, z, hlogits, sel, sel_bytes, attn_scratch, total;
+  int64_t codes, scales, gate_up, i8_ws, i8_ws_bytes;  // 8-bit models: a product's rows, the gate/up product, a product's scratch
   int max_slots;  // partial-sum slots that `part` holds for each of a layer's GEMMs
 };
 
@@ -176,7 +177,17 @@ static Workspace carve(const mdz_model_desc& m, int B, int max_prefix, bool laye
   {
     int64_t layer_part = 0;
     const int shapes[4][2] = {{m.d + 2 * kv_width(m), m.d}, {m.d, m.d}, {2 * m.ffn, m.d}, {m.d, m.ffn}};
-    for (auto& sh : shapes) {
+    if (m.weights_i8) {  // the finished products of QKV, and of O and down
+      layer_part = rows * (m.d + 2 * kv_width(m)) * 4;
+      w.codes = take(rows * (m.d > m.ffn ? m.d : m.ffn));
+      w.scales = take(rows * 4);
+      w.gate_up = take(rows * 2 * m.ffn * es);
+      for (auto& sh : shapes) {
+        const int64_t b = medusa_linear_i8_workspace_bytes((int)rows, sh[0], sh[1]);
+        w.i8_ws_bytes = b > w.i8_ws_bytes ? b : w.i8_ws_bytes;
+      }
+      w.i8_ws = take(w.i8_ws_bytes);
+    } else for (auto& sh : shapes) {
       int64_t e = gemm_part_elems(m.dtype, (int)rows, sh[0], sh[1], max_slots) * 4;
       layer_part = e > layer_part ? e : layer_part;
     }
@@ -227,6 +238,11 @@ static int check_model(const mdz_model_desc* m) {
   MDZ_REQUIRE(m->rms_eps >= 0.f && m->rope_base > 1.f, MDZ_EINVAL, "bad rms_eps / rope_base");
   MDZ_REQUIRE(m->ffn_f16 == 0 || (m->ffn_f16 == 1 && m->dtype == MDZ_BF16), MDZ_EINVAL,
               "ffn_f16 is 0 or 1 and applies to bf16 models only (ffn_f16 %d, dtype %d)", m->ffn_f16, m->dtype);
+  MDZ_REQUIRE(m->weights_i8 == 0 || (m->weights_i8 == 1 && is_16bit(m->dtype) && m->ffn_f16 == 0), MDZ_EINVAL,
+              "weights_i8 is 0 or 1 and applies to bf16 and fp16 models without ffn_f16 (weights_i8 %d, dtype %d, ffn_f16 %d)", m->weights_i8,
+              m->dtype, m->ffn_f16);
+  MDZ_REQUIRE(m->weights_i8 == 0 || (m->d <= 131071 && m->ffn <= 131071), MDZ_EUNSUPPORTED,
+              "weights_i8: d %d and ffn %d: up to 131071 input features, whose 32-bit sums cannot overflow", m->d, m->ffn);
   return MDZ_OK;
 }
 
@@ -262,6 +278,53 @@ static int check_kv(const mdz_model_desc* m, const mdz_kv_desc* kv, int B, int m
 static KvGeom geom(const mdz_kv_desc* kv, int group = 1) {
   return KvGeom{kv->n_layers, kv->batch, kv->n_heads, kv->head_dim, kv->cap,
                 (is_16bit(kv->dtype) && kv->head_dim % 32 == 0) ? 1 : 0, group, kv->quant == MDZ_KV_FP8E4M3 ? 1 : 0};
+}
+
+// The layer of an 8-bit model.  On entry ws.codes and ws.scales hold RMSNorm(x; g_attn) in 8 bits.  Where another layer follows (xn_next is
+// NULL and g_next is not) they hold its normalised input on return; else xn_next as in run_layer.
+static int run_layer_i8(const mdz_model_desc& m, const mdz_layer_weights& lw, int layer, float* x, const mdz_kv_desc* kv,
+                        const int32_t* seq_len, int B, int max_prefix, char* ws, const Workspace& w, const void* g_next, void* xn_next,
+                        hipStream_t st) {
+  const int rows = B * host_tree(m.tree)->T;
+  const KvGeom g = geom(kv, m.n_heads / kv_heads(m));
+  const int qkv_cols = m.d + 2 * kv_width(m);
+  int8_t* codes = (int8_t*)(ws + w.codes);
+  float* scales = (float*)(ws + w.scales);
+  float* part = (float*)(ws + w.part);
+  void* att = ws + w.att;
+  void* gu = ws + w.gate_up;
+  void* i8_ws = ws + w.i8_ws;
+  int rc;
+  auto product = [&](const void* packed, int N, int K, int dtype, void* y) {
+    return medusa_linear_i8(codes, scales, packed, rows, N, K, dtype, y, i8_ws, w.i8_ws_bytes, st);
+  };
+  if ((rc = product(lw.wqkv, qkv_cols, m.d, MDZ_FP32, part))) return rc;
+  if ((rc = launch_rope_attention(m.dtype, m.tree, single_slot(part, (int64_t)rows * qkv_cols, qkv_cols), (float*)(ws + w.rope_cs), ws + w.q,
+                                  g, kv->k, kv->v, layer, seq_len, B, max_prefix, att, ws + w.attn_scratch, w.total - w.attn_scratch, st)))
+    return rc;
+  if ((rc = medusa_quantize_rows_i8(m.dtype, att, rows, m.d, codes, scales, nullptr, st))) return rc;
+  if ((rc = product(lw.wo, m.d, m.d, MDZ_FP32, part))) return rc;
+  if ((rc = medusa_residual_rmsnorm_i8(m.dtype, x, part, MDZ_FP32, lw.g_ffn, m.rms_eps, rows, m.d, x, codes, scales, nullptr, st))) return rc;
+  if ((rc = product(lw.wgateup, 2 * m.ffn, m.d, m.dtype, gu))) return rc;
+  if ((rc = medusa_swiglu_i8(m.dtype, gu, rows, m.ffn, codes, scales, nullptr, st))) return rc;
+  if ((rc = product(lw.wdown, m.d, m.ffn, MDZ_FP32, part))) return rc;
+  if (g_next && !xn_next)
+    return medusa_residual_rmsnorm_i8(m.dtype, x, part, MDZ_FP32, g_next, m.rms_eps, rows, m.d, x, codes, scales, nullptr, st);
+  return launch_residual_rmsnorm(m.dtype, x, single_slot(part, (int64_t)rows * m.d, m.d), g_next, xn_next, rows, m.d, m.rms_eps, st);
+}
+
+// What opens a pass: the RoPE table, and RMSNorm(x; g) in ws.xn, or in ws.codes and ws.scales for an 8-bit model.
+static int open_pass(const mdz_model_desc& m, float* x, const void* g, const mdz_kv_desc* kv, const int32_t* seq_len, int B, int max_prefix,
+                     char* ws, const Workspace& w, hipStream_t st) {
+  const int rows = B * host_tree(m.tree)->T;
+  float* cs = (float*)(ws + w.rope_cs);
+  if (!m.weights_i8)
+    return launch_first_norm_and_rope_table(m.dtype, x, g, ws + w.xn, rows, m.d, m.rms_eps, m.tree, seq_len, B, max_prefix, m.head_dim,
+                                            m.rope_base, cs, kv->status, st);
+  int rc = launch_rope_table(m.tree, seq_len, B, max_prefix, m.head_dim, m.rope_base, cs, kv->status, st);
+  if (rc) return rc;
+  return medusa_residual_rmsnorm_i8(m.dtype, x, nullptr, MDZ_FP32, g, m.rms_eps, rows, m.d, nullptr, (int8_t*)(ws + w.codes),
+                                    (float*)(ws + w.scales), nullptr, st);
 }
 
 // One decoder layer over rows = B*T rows of x.  On entry ws.xn holds RMSNorm(x; g_attn of this layer).  The
@@ -341,6 +404,16 @@ static int static_scratch(void** out) {
 static int check_layer_weights(const mdz_layer_weights* lw) {
   MDZ_REQUIRE(lw && lw->wqkv && lw->wo && lw->wgateup && lw->wdown && lw->g_attn && lw->g_ffn, MDZ_EINVAL,
               "layer weights: NULL pointer");
+  return MDZ_OK;
+}
+
+// The 8-bit products' demands on a caller's buffers, asked before anything is enqueued (other models take any alignment).
+static int check_i8_buffers(const mdz_model_desc& m, const mdz_layer_weights& lw, const void* ws) {
+  if (!m.weights_i8) return MDZ_OK;
+  MDZ_REQUIRE(aligned16(lw.wqkv, lw.wo) && aligned16(lw.wgateup, lw.wdown), MDZ_EINVAL, "weights_i8: packed matrices must start on 16 bytes");
+  MDZ_REQUIRE(((reinterpret_cast<uintptr_t>(lw.g_attn) | reinterpret_cast<uintptr_t>(lw.g_ffn)) & 1) == 0, MDZ_EINVAL,
+              "weights_i8: gains must be aligned to their elements");
+  MDZ_REQUIRE(aligned16(ws, ws), MDZ_EINVAL, "weights_i8: the workspace must start on 16 bytes");
   return MDZ_OK;
 }
 
@@ -601,19 +674,17 @@ static int verify_layer_checked(const mdz_model_desc* model, const mdz_layer_wei
               layer, kv->n_layers);
   MDZ_REQUIRE(max_prefix + t->T <= kv->cap, MDZ_ESHAPE, "max_prefix %d + T %d exceeds kv cap %d", max_prefix, t->T,
               kv->cap);
+  MDZ_REQUIRE(!model->weights_i8 || (reinterpret_cast<uintptr_t>(x_inout) & 3) == 0, MDZ_EINVAL,
+              "weights_i8: x must be aligned to its elements");
   return MDZ_OK;
 }
 
 static int verify_layer_run(const mdz_model_desc* model, const mdz_layer_weights* lw, int layer, float* x_inout,
                             const mdz_kv_desc* kv, const int32_t* seq_len, int B, int max_prefix, char* ws,
                             const Workspace& L, hipStream_t st) {
-  int rc;
-  const TreeTables* t = host_tree(model->tree);
-  const int rows = B * t->T;
-  if ((rc = launch_first_norm_and_rope_table(model->dtype, x_inout, lw->g_attn, ws + L.xn, rows, model->d, model->rms_eps,
-                                             model->tree, seq_len, B, max_prefix, model->head_dim, model->rope_base,
-                                             (float*)(ws + L.rope_cs), kv->status, st)))
-    return rc;
+  const int rc = open_pass(*model, x_inout, lw->g_attn, kv, seq_len, B, max_prefix, ws, L, st);
+  if (rc) return rc;
+  if (model->weights_i8) return run_layer_i8(*model, *lw, layer, x_inout, kv, seq_len, B, max_prefix, ws, L, nullptr, nullptr, st);
   return run_layer(*model, *lw, layer, x_inout, kv, seq_len, B, max_prefix, ws, L, nullptr, nullptr, st);
 }
 
@@ -626,6 +697,7 @@ int tree_verify_layer(const mdz_model_desc* model, const mdz_layer_weights* lw, 
   const Workspace L = carve(*model, B, max_prefix);
   MDZ_REQUIRE(ws_bytes >= L.total, MDZ_EWORKSPACE, "tree_verify_layer: workspace %lld < %lld bytes",
               (long long)ws_bytes, (long long)L.total);
+  if ((rc = check_i8_buffers(*model, *lw, ws))) return rc;
   if (B == 0) return MDZ_OK;
   return verify_layer_run(model, lw, layer, x_inout, kv, seq_len, B, max_prefix, (char*)ws, L, (hipStream_t)stream);
 }
@@ -643,6 +715,7 @@ int tree_verify_layer_static(const mdz_model_desc* model, const mdz_layer_weight
               "tree_verify_layer_static: this shape (B %d, max_prefix %d) needs %lld bytes of scratch, the built-in buffer "
               "holds %lld; use tree_verify_layer with a caller workspace",
               B, max_prefix, (long long)L.total, (long long)kStaticScratchBytes);
+  if ((rc = check_i8_buffers(*model, *lw, nullptr))) return rc;
   if (B == 0) return MDZ_OK;
   void* ws = nullptr;
   if ((rc = static_scratch(&ws))) return rc;
@@ -667,6 +740,8 @@ int tree_verify_step(const mdz_model_desc* model, const mdz_weights* w, const in
   const Workspace L = carve(m, B, max_prefix);
   MDZ_REQUIRE(ws_bytes >= L.total, MDZ_EWORKSPACE, "tree_verify_step: workspace %lld < %lld bytes",
               (long long)ws_bytes, (long long)L.total);
+  for (int l = 0; l < m.n_layers; ++l)
+    if ((rc = check_i8_buffers(m, w->layers[l], ws))) return rc;
   if (B == 0) return MDZ_OK;
   hipStream_t st = (hipStream_t)stream;
   char* wsb = (char*)ws;
@@ -678,11 +753,15 @@ int tree_verify_step(const mdz_model_desc* model, const mdz_weights* w, const in
   // need aligned operands (1024 rows x 128000 columns: 0.88 ms, 1.56 on the unaligned rows; the copy takes about 10 us).
   const bool copy_hidden = hidden_out && !aligned16(hidden_out, hidden_out) && gemm_tile_supported(m.dtype, rows, m.vocab, m.d);
   void* hid = hidden_out && !copy_hidden ? hidden_out : xn;
-  if ((rc = launch_first_norm_and_rope_table(m.dtype, x, w->layers[0].g_attn, xn, rows, m.d, m.rms_eps, m.tree, seq_len, B,
-                                             max_prefix, m.head_dim, m.rope_base, (float*)(wsb + L.rope_cs), kv->status, st)))
-    return rc;
+  if ((rc = open_pass(m, x, w->layers[0].g_attn, kv, seq_len, B, max_prefix, wsb, L, st))) return rc;
   for (int l = 0; l < m.n_layers; ++l) {
     const bool last = l + 1 == m.n_layers;
+    if (m.weights_i8) {
+      if ((rc = run_layer_i8(m, w->layers[l], l, x, kv, seq_len, B, max_prefix, wsb, L, last ? w->g_final : w->layers[l + 1].g_attn,
+                             last ? hid : nullptr, st)))
+        return rc;
+      continue;
+    }
     if ((rc = run_layer(m, w->layers[l], l, x, kv, seq_len, B, max_prefix, wsb, L,
                         last ? w->g_final : w->layers[l + 1].g_attn, last ? hid : xn, st)))
       return rc;

@@ -21,10 +21,10 @@ class DeviceModel:
     """Packed weights of one decoder (+ Medusa heads) on one GPU."""
 
     def __init__(self, *, d, n_heads, head_dim, ffn, vocab, n_layers, dtype: str, tree: str, n_kv_heads: int = 0, rms_eps=1e-5,
-                 rope_base=10000.0, device="cuda:0", ffn_f16: bool = False):
+                 rope_base=10000.0, device="cuda:0", ffn_f16: bool = False, weights_i8: bool = False):
         self.desc = B.ModelDesc(d, n_heads, head_dim, ffn, vocab, n_layers, B.DTYPES[dtype], B.TREES[tree], rms_eps,
-                                rope_base, n_kv_heads, int(ffn_f16))
-        self.ffn_f16 = bool(ffn_f16)
+                                rope_base, n_kv_heads, int(ffn_f16), int(weights_i8))
+        self.ffn_f16, self.weights_i8 = bool(ffn_f16), bool(weights_i8)
         self.kv_heads = n_kv_heads or n_heads
         self.device = torch.device(device)
         self.dtype = B.DTYPES[dtype]
@@ -68,6 +68,20 @@ class DeviceModel:
         torch.cuda.synchronize(self.device)          # the row-major sources may be freed by the caller now
         return dst
 
+    def pack_i8(self, mats: Sequence[torch.Tensor]) -> torch.Tensor:
+        """Stacks row-major [n_i, k] matrices into one packed 8-bit matrix, quantised per row."""
+        k, total = mats[0].shape[1], sum(m.shape[0] for m in mats)
+        dst = torch.empty(B.medusa_packed_i8_bytes(total, k), dtype=torch.uint8, device=self.device)
+        self._keep.append(dst)
+        self.packed_bytes += dst.numel()
+        off = 0
+        for m in mats:
+            m = self._dev(m)
+            B.medusa_pack_weight_i8(m, dst, total, off // B.MDZ_I8_TILE_ROWS)
+            off += m.shape[0]
+        torch.cuda.synchronize(self.device)          # the row-major sources may be freed by the caller now
+        return dst
+
     def _gain(self, g) -> torch.Tensor:
         g = self._dev(g)
         self._keep.append(g)
@@ -75,10 +89,12 @@ class DeviceModel:
 
     # -- model assembly --------------------------------------------------------------------------
     def add_layer(self, wq, wk, wv, wo, wgate, wup, wdown, g_attn, g_ffn) -> None:
-        lw = B.LayerWeights(self.pack([wq, wk, wv]).data_ptr(), self.pack([wo]).data_ptr(),
-                            self.pack([wgate, wup], interleave=True, as_f16=self.ffn_f16).data_ptr(),
-                            self.pack([wdown], as_f16=self.ffn_f16).data_ptr(),
-                            self._gain(g_attn).data_ptr(), self._gain(g_ffn).data_ptr())
+        if self.weights_i8:
+            mats = [self.pack_i8(m) for m in ([wq, wk, wv], [wo], [wgate, wup], [wdown])]
+        else:
+            mats = [self.pack([wq, wk, wv]), self.pack([wo]), self.pack([wgate, wup], interleave=True, as_f16=self.ffn_f16),
+                    self.pack([wdown], as_f16=self.ffn_f16)]
+        lw = B.LayerWeights(*[m.data_ptr() for m in mats], self._gain(g_attn).data_ptr(), self._gain(g_ffn).data_ptr())
         self._layers.append(lw)
 
     def set_embed(self, e) -> None:
@@ -133,7 +149,7 @@ class DeviceModel:
         other = copy.copy(self)
         d = self.desc
         other.desc = B.ModelDesc(d.d, d.n_heads, d.head_dim, d.ffn, d.vocab, d.n_layers, d.dtype, B.TREES[tree],
-                                 d.rms_eps, d.rope_base, d.n_kv_heads, d.ffn_f16)
+                                 d.rms_eps, d.rope_base, d.n_kv_heads, d.ffn_f16, d.weights_i8)
         other.tree = B.TREES[tree]
         other.tree_info = B.medusa_tree_info(other.tree)
         keep = len(self._heads) if other.tree_info["K"] == len(self._heads) else 0

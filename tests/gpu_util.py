@@ -17,7 +17,7 @@ def device_model(w: W.Workload, heads: bool = True, n_layers=None, gen_device=DE
     L = w.n_layers if n_layers is None else n_layers
     dm = DeviceModel(d=w.d, n_heads=w.n_heads, head_dim=w.head_dim, ffn=w.ffn, vocab=w.vocab, n_layers=L,
                      dtype=w.dtype, tree=w.tree.name, n_kv_heads=w.n_kv_heads, rms_eps=w.rms_eps, rope_base=w.rope_base, device=DEV,
-                     ffn_f16=w.ffn_f16)
+                     ffn_f16=w.ffn_f16, weights_i8=w.weights_i8)
     for l in range(L):
         mats = [W.layer_weight(w, l, m, gen_device) for m in W.LAYER_MATS]
         dm.add_layer(*mats, W.norm_gain(w, f"layer{l}.g_attn", gen_device), W.norm_gain(w, f"layer{l}.g_ffn", gen_device))

@@ -149,3 +149,16 @@ def test_binding_refuses_shapes_and_types():
             assert e.status in (-1, -2), (k, e)
         else:
             pytest.fail(f"call {k} was not refused")
+
+
+def test_model_option():
+    ok = P.ModelDesc(256, 4, 64, 704, 1024, 2, P.MDZ_BF16, P.MDZ_TREE_15, 1e-5, 1e4, 0, 0, 1)
+    plain = P.ModelDesc(256, 4, 64, 704, 1024, 2, P.MDZ_BF16, P.MDZ_TREE_15, 1e-5, 1e4)
+    assert P.medusa_workspace_bytes(ok, 1, 64) > 0 and plain.weights_i8 == 0
+    for dtype, f16, i8 in [(P.MDZ_FP32, 0, 1), (P.MDZ_BF16, 1, 1), (P.MDZ_FP16, 0, 2), (P.MDZ_BF16, 0, -1)]:
+        with pytest.raises(P.MedusaError) as e:
+            P.medusa_workspace_bytes(P.ModelDesc(256, 4, 64, 704, 1024, 2, dtype, P.MDZ_TREE_15, 1e-5, 1e4, 0, f16, i8), 1, 64)
+        assert e.value.status == -1
+    with pytest.raises(P.MedusaError) as e:  # sums over so many features could overflow
+        P.medusa_workspace_bytes(P.ModelDesc(256, 4, 64, 131072, 1024, 2, P.MDZ_BF16, P.MDZ_TREE_15, 1e-5, 1e4, 0, 0, 1), 1, 64)
+    assert e.value.status == -3
