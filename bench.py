@@ -51,6 +51,8 @@ def algorithmic_bytes(w, with_heads: bool):
     T, K = w.tree.n_nodes, w.n_medusa
     kvd = w.kv_heads * w.head_dim
     layer_w = (2 * w.d * w.d + 2 * kvd * w.d + 3 * w.d * w.ffn) * es
+    if w.weights_i8:  # a byte each, and one fp32 scale per output feature
+        layer_w = layer_w // es + 4 * (3 * w.d + 2 * kvd + 2 * w.ffn)
     gemm_layers = w.n_layers * layer_w
     lm = w.vocab * w.d * es
     heads = K * (w.d * w.d + w.vocab * w.d) * es if with_heads else 0
@@ -59,7 +61,7 @@ def algorithmic_bytes(w, with_heads: bool):
     kv_prefix = sum(w.prefix) * kv_row * w.n_layers
     kv_tree = 2 * w.batch * T * kv_row * w.n_layers               # written + read
     embed = w.batch * T * w.d * es
-    gemm_w64 = gemm_layers + lm          # every 64-row launch: QKV, O, gate/up, down of each layer and the LM head
+    gemm_w64 = (0 if w.weights_i8 else gemm_layers) + lm  # every 16-bit 64-row launch: QKV, O, gate/up, down of each layer and the LM head
     return dict(gemm=gemm_layers + lm + heads, gemm_w64=gemm_w64,
                 weights_layers=gemm_layers, lm_head=lm, heads=heads,
                 kv_prefix=kv_prefix, kv_tree=kv_tree, embed=embed,
@@ -73,7 +75,7 @@ def build_device(w, with_heads):
     dev = "cuda:0"
     dm = P.DeviceModel(d=w.d, n_heads=w.n_heads, head_dim=w.head_dim, ffn=w.ffn, vocab=w.vocab, n_layers=w.n_layers,
                        dtype=w.dtype, tree=w.tree.name, n_kv_heads=w.n_kv_heads, rms_eps=w.rms_eps, rope_base=w.rope_base, device=dev,
-                       ffn_f16=w.ffn_f16)
+                       ffn_f16=w.ffn_f16, weights_i8=w.weights_i8)
     for l in range(w.n_layers):
         mats = [W.layer_weight(w, l, m, dev) for m in W.LAYER_MATS]
         dm.add_layer(*mats, W.norm_gain(w, f"layer{l}.g_attn", dev), W.norm_gain(w, f"layer{l}.g_ffn", dev))
@@ -311,6 +313,8 @@ def main():
     ap.add_argument("--kv8", action="store_true", help="8-bit KV cache rows (E4M3 codes + one fp32 scale per row)")
     ap.add_argument("--ffn-f16", action="store_true",
                     help="bf16 model with binary16 feed-forward operands (the model descriptor's ffn_f16 option)")
+    ap.add_argument("--weights-i8", action="store_true",
+                    help="8-bit integer products in the layers (the model descriptor's weights_i8 option)")
     ap.add_argument("--skip-cpu-baseline", action="store_true")
     ap.add_argument("--skip-extras", action="store_true",
                     help="leave out the autoregressive baseline, the chained loop and the other configurations "
@@ -330,6 +334,8 @@ def main():
         w = w.with_(name=f"{w.name}+kv8", kv_quant="fp8e4m3")
     if args.ffn_f16:
         w = w.with_(name=f"{w.name}+ffn_f16", ffn_f16=True)
+    if args.weights_i8:
+        w = w.with_(name=f"{w.name}+weights_i8", weights_i8=True)
     if args.prefix is not None:
         w = w.with_(name=f"{w.name}@prefix{args.prefix}", prefix=(args.prefix,) * w.batch)
     with_heads = not args.no_heads and w.n_layers > 1
@@ -426,7 +432,7 @@ def main():
 
     # configs 2, 4 and 5 on the same weights (default headline run only)
     others = None
-    if args.workload == "cfg3_step_1k" and not (args.skip_extras or args.kv8 or args.ffn_f16 or args.no_heads or args.prefix is not None):
+    if args.workload == "cfg3_step_1k" and not (args.skip_extras or args.kv8 or args.ffn_f16 or args.weights_i8 or args.no_heads or args.prefix is not None):
         del kv, buf
         torch.cuda.empty_cache()
         others = other_configs(dm, w, args.steps, args.warmup)

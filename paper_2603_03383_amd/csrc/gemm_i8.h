@@ -51,5 +51,6 @@ constexpr int kNumI8Tiles = 9;
 extern const I8Tile kI8Tiles[kNumI8Tiles];
 // The features in `splits` parts: more than one write their 32-bit sums to `partial` (splits x M x 16 n_tiles), and a second launch adds them.
 int launch_i8_tile(int out_dtype, const I8Product& p, int tile, int splits, void* partial, hipStream_t st);
+int launch_i8_tile_parts(const I8Product& p, int tile, int splits, void* partial, hipStream_t st);  // the first launch alone
 
 }  // namespace mdz

@@ -110,7 +110,8 @@ struct I8Plan {
 // of what a CU needs for its workgroups, what the chip needs for all, and W from HBM, which idle CUs slow down; a split adds a launch and
 // its sums' way to memory and back.  Fitted to 2300 timings (1 .. 2048 rows, 688 x 256 .. 22016 x 4096 and 5120 x 13824): what it picks
 // takes 0.8 % longer than the best of them on average, and 13 % at most where a launch takes more than 5 us.
-static I8Plan plan_i8(int M, int N, int K) {
+// summed_later: the consumer adds the parts, so a split costs no launch, and has up to kI8MaxParts.
+static I8Plan plan_i8(int M, int N, int K, bool summed_later = false) {
   I8Plan best{-1, 1, 0, 0};
   if (M <= 16 || (M <= 32 && K <= 8192 && (int64_t)N * K <= 1 << 26)) return best;
   const int n_pad = (int)i8_padded_rows(N), stages = (K + 127) / 128, cus = num_cus();
@@ -121,13 +122,13 @@ static I8Plan plan_i8(int M, int N, int K) {
     if (t > 0 && tile.rows >= 2 * M) break;
     const int64_t blocks = (int64_t)((M + tile.rows - 1) / tile.rows) * ((N + tile.cols - 1) / tile.cols);
     for (int splits : {1, 2, 3, 4, 6, 8}) {
-      if (splits > 1 && (splits * 4 > stages || blocks * splits > 4 * cus)) break;
+      if (splits > 1 && (splits * 4 > stages || blocks * splits > 4 * cus || (summed_later && splits > kI8MaxParts))) break;
       const int64_t wgs = blocks * splits;
       const float s = (float)((stages + splits - 1) / splits);
       const float rounds = (float)((wgs + cus - 1) / cus);
       const float cu = rounds * s * tile.us_stage * (rounds > 1.f && tile.two ? 0.81f : 1.f);
       float us = fmaxf(fmaxf(cu, (float)wgs * s * tile.us_all), hbm * sqrtf(rounds * cus / wgs)) + 0.36f * (rounds - 1.f);
-      if (splits > 1) us += 2.f + (float)splits * M * n_pad * (4e-6f / 2.5f);
+      if (splits > 1) us += (summed_later ? 0.f : 2.f) + (float)splits * M * n_pad * (4e-6f / 2.5f);
       if (best.tile < 0 || us < least) best.tile = t, best.splits = splits, least = us;
     }
   }
@@ -152,6 +153,40 @@ static int check_linear_i8(int M, int N, int K) {
   MDZ_REQUIRE(M >= 0 && N > 0 && K > 0, MDZ_EINVAL, "linear_i8: [%d,%d] x [%d,%d]", M, K, N, K);
   MDZ_REQUIRE(K <= kI8MaxK, MDZ_EUNSUPPORTED, "linear_i8: up to %d input features, whose 32-bit sums cannot overflow (%d)", kI8MaxK, K);
   MDZ_REQUIRE((int64_t)M * N < (int64_t)1 << 40 && N <= INT32_MAX - kI8TileRows, MDZ_EUNSUPPORTED, "linear_i8: %d x %d outputs", M, N);
+  return MDZ_OK;
+}
+
+static I8Product describe(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, void* y, int out_bytes) {
+  I8Product p{};
+  p.X = codes, p.sx = scales, p.W = (const uint8_t*)packed, p.sw = (const float*)((const char*)packed + i8_scales_offset(N, K)), p.Y = y;
+  p.M = M, p.N = N, p.K = K, p.ldx = K, p.kp = i8_padded_k(K), p.n_tiles = (int)(i8_padded_rows(N) / kI8TileRows);
+  p.quads = N % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * out_bytes) == 0;
+  return p;
+}
+
+// The tiles' loads take 16 bytes from addresses of 16: rows that do not start there go through the workspace.
+static int align_rows(I8Product& p, const I8Plan& plan, void* ws, hipStream_t st) {
+  if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.X) % 16 == 0) return MDZ_OK;
+  i32x4* aligned = (i32x4*)((char*)ws + plan.aligned_at);
+  const int64_t chunks = (int64_t)p.M * (p.kp / 16);
+  launch_timed(PROF_GEMM_I8, align_rows_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, p.X, p.K, aligned, chunks, (int)(p.kp / 16));
+  MDZ_LAUNCH_CHECK();
+  p.X = (const int8_t*)aligned, p.ldx = p.kp, p.K = (int)p.kp;
+  return MDZ_OK;
+}
+
+int64_t linear_i8_parts_bytes(int M, int N, int K) { return plan_i8(M, N, K, true).bytes; }
+
+int launch_linear_i8_parts(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, float* y, void* ws, int64_t ws_bytes,
+                           I8Sums* sums, hipStream_t st) {
+  *sums = I8Sums{};
+  const I8Plan plan = plan_i8(M, N, K, true);
+  if (plan.splits == 1) return medusa_linear_i8(codes, scales, packed, M, N, K, MDZ_FP32, y, ws, ws_bytes, st);
+  MDZ_REQUIRE(ws_bytes >= plan.bytes, MDZ_EWORKSPACE, "linear_i8: workspace %lld < %lld bytes", (long long)ws_bytes, (long long)plan.bytes);
+  I8Product p = describe(codes, scales, packed, M, N, K, y, 4);
+  int rc = align_rows(p, plan, ws, st);
+  if (rc || (rc = launch_i8_tile_parts(p, plan.tile, plan.splits, ws, st))) return rc;
+  *sums = I8Sums{(const int32_t*)ws, plan.splits, p.n_tiles * 16, (int64_t)M * p.n_tiles * 16, scales, p.sw};
   return MDZ_OK;
 }
 
@@ -192,18 +227,9 @@ int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packe
               (long long)ws_bytes, (long long)plan.bytes);
   MDZ_REQUIRE(plan.bytes == 0 || (reinterpret_cast<uintptr_t>(ws) & 15) == 0, MDZ_EINVAL, "linear_i8: the workspace must start on 16 bytes");
   hipStream_t st = (hipStream_t)stream;
-  I8Product p{};
-  p.X = codes, p.sx = scales, p.W = (const uint8_t*)packed, p.sw = (const float*)((const char*)packed + i8_scales_offset(N, K)), p.Y = y;
-  p.M = M, p.N = N, p.K = K, p.ldx = K, p.kp = i8_padded_k(K), p.n_tiles = (int)(i8_padded_rows(N) / kI8TileRows);
-  p.quads = N % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * elem_bytes(out_dtype)) == 0;
+  I8Product p = describe(codes, scales, packed, M, N, K, y, elem_bytes(out_dtype));
   if (plan.tile < 0) MDZ_WITH_ELEM(out_dtype, return (M <= 16 ? launch_few_rows<1, E>(p, st) : launch_few_rows<2, E>(p, st)));
-  if (K % 16 != 0 || reinterpret_cast<uintptr_t>(codes) % 16 != 0) {  // the tiles' loads take 16 bytes from addresses of 16
-    i32x4* aligned = (i32x4*)((char*)ws + plan.aligned_at);
-    const int64_t chunks = (int64_t)M * (p.kp / 16);
-    launch_timed(PROF_GEMM_I8, align_rows_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, codes, K, aligned, chunks, (int)(p.kp / 16));
-    MDZ_LAUNCH_CHECK();
-    p.X = (const int8_t*)aligned, p.ldx = p.kp, p.K = (int)p.kp;
-  }
+  if ((rc = align_rows(p, plan, ws, st))) return rc;
   return launch_i8_tile(out_dtype, p, plan.tile, plan.splits, ws, st);
 }
 

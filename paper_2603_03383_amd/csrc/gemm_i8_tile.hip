@@ -172,9 +172,13 @@ static int launch_by_tile(const I8Product& p, int tile, int splits, i32x4* parti
   MDZ_FAIL(MDZ_EINVAL, "linear_i8: no tile %d", tile);
 }
 
+int launch_i8_tile_parts(const I8Product& p, int tile, int splits, void* partial, hipStream_t st) {
+  return launch_by_tile<float, true>(p, tile, splits, (i32x4*)partial, st);
+}
+
 int launch_i8_tile(int out_dtype, const I8Product& p, int tile, int splits, void* partial, hipStream_t st) {
   if (splits == 1) MDZ_WITH_ELEM(out_dtype, return (launch_by_tile<E, false>(p, tile, 1, nullptr, st)));
-  int rc = launch_by_tile<float, true>(p, tile, splits, (i32x4*)partial, st);
+  const int rc = launch_i8_tile_parts(p, tile, splits, partial, st);
   if (rc) return rc;
   const int64_t quads = (int64_t)p.M * p.n_tiles * 4;
   MDZ_WITH_ELEM(out_dtype, (launch_timed(PROF_GEMM_I8, gemm_i8_finish_kernel<E>, (unsigned)((quads + 255) / 256), 256, 0, st, p,

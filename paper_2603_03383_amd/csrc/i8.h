@@ -58,4 +58,25 @@ __host__ __device__ inline int64_t i8_index(int64_t n, int64_t k, int64_t kp) {
   return (n >> 4) * 16 * kp + (k >> 6) * 1024 + ((n & 15) + 16 * ((k >> 4) & 3)) * 16 + (k & 15);
 }
 
+// ---- a layer's products and norms (medusa_api.hip) ---------------------------------------------------
+// A product whose features were cut into parts, as its consumer adds it up: y[m][n] = sx[m] * sw[n] * sum of parts[s][m][n], s < n.  n == 0: the
+// product is finished.
+constexpr int kI8MaxParts = 4;
+struct I8Sums {
+  const int32_t* parts;
+  int n, ld;
+  int64_t stride;
+  const float* sx;
+  const float* sw;
+};
+// medusa_linear_i8 into y, or, where that is faster, parts in ws and no second launch; bit for bit the same numbers
+int launch_linear_i8_parts(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, float* y, void* ws, int64_t ws_bytes,
+                           I8Sums* sums, hipStream_t st);
+int64_t linear_i8_parts_bytes(int M, int N, int K);
+// medusa_residual_rmsnorm_i8 in place with such a product as the update (delta where sums.n == 0); parts need d <= kI8MaxPartsWidth and a multiple
+// of four
+constexpr int kI8MaxPartsWidth = 16384;
+int launch_residual_rmsnorm_i8(int dtype, float* x, const float* delta, const I8Sums& sums, const void* gain, float eps, int rows, int d,
+                               int8_t* codes, float* scales, hipStream_t st);
+
 }  // namespace mdz

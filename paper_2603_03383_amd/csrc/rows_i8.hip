@@ -196,6 +196,51 @@ struct NormRows {
   }
 };
 
+// the same with the update still in parts: finished here as the product's own second launch would
+template <typename E>
+struct NormOfSumsRows {
+  static constexpr int kW = 4;
+  typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+  struct Raw {
+    Elems<float, kW> x, sw;
+    Elems<E, kW> gain;
+    i32x4 part[kI8MaxParts];
+    float sx;
+  };
+  float* x;
+  I8Sums sums;
+  const E* gain;
+  int d;
+  float eps;
+  template <bool TAIL>
+  __device__ inline void load(int64_t r, int i, int n, Raw& raw) const {
+    raw.x = fetch<TAIL, kW>(x + r * d + i, n);
+#pragma unroll
+    for (int s = 0; s < kI8MaxParts; ++s)
+      if (s < sums.n) raw.part[s] = *reinterpret_cast<const i32x4*>(sums.parts + s * sums.stride + r * sums.ld + i);
+    raw.sx = sums.sx[r];
+    raw.sw = fetch<TAIL, kW>(sums.sw + i, n);
+    raw.gain = fetch<TAIL, kW>(gain + i, n);
+  }
+  template <bool TAIL>
+  __device__ inline void values(int64_t r, int i, int n, const Raw& raw, float (&t)[kW], float& squares) const {
+#pragma clang fp contract(off)  // every rounding as where the product is stored in between
+    i32x4 sum = raw.part[0];
+#pragma unroll
+    for (int s = 1; s < kI8MaxParts; ++s)
+      if (s < sums.n) sum += raw.part[s];
+    Elems<float, kW> y;
+#pragma unroll
+    for (int e = 0; e < kW; ++e) {
+      y.v[e] = raw.x.v[e] + (float)sum[e] * (raw.sx * raw.sw.v[e]);
+      squares += n > 0 ? y.v[e] * y.v[e] : 0.f;
+      t[e] = y.v[e] * to_float(raw.gain.v[e]);
+    }
+    if (n > 0) put<TAIL, kW>(x + r * d + i, n, y);
+  }
+  __device__ inline float factor(float squares) const { return 1.f / sqrtf(squares / (float)d + eps); }
+};
+
 // codes of t and what they stand for, W at a time
 template <bool TAIL, typename E, int W>
 __device__ inline void put_codes(const I8Quantiser& q, const float (&t)[W], int n, float scale, int8_t* codes, E* values) {
@@ -274,7 +319,8 @@ template <typename E, bool TAIL, typename Rows>
 static auto rows_i8_variant(const Rows&, int nv) {
   return nv == 1 ? rows_i8_kernel<Rows, E, 1, TAIL> : nv == 2 ? rows_i8_kernel<Rows, E, 2, TAIL> : rows_i8_kernel<Rows, E, 4, TAIL>;
 }
-template <typename E, typename Rows>
+// ANY: any width; else whole pieces that fit the registers of a workgroup
+template <typename E, bool ANY, typename Rows>
 static int launch_rows_i8(const Rows& in, int rows, int d, int8_t* codes, float* scales, void* values, hipStream_t st) {
   if (rows == 0) return MDZ_OK;
   const int pieces = (d + Rows::kW - 1) / Rows::kW;
@@ -284,11 +330,22 @@ static int launch_rows_i8(const Rows& in, int rows, int d, int8_t* codes, float*
   const int most = rows <= num_cus() ? 1024 : 256;
   const int nv = pieces <= most ? 1 : pieces <= 2 * most ? 2 : 4;
   int threads = ((pieces + nv - 1) / nv + 63) / 64 * 64;
-  auto kernel = d % Rows::kW ? rows_i8_variant<E, true>(in, nv) : rows_i8_variant<E, false>(in, nv);
-  if (pieces > 4096) kernel = rows_i8_long_kernel<Rows, E>, threads = 1024;
+  auto kernel = rows_i8_variant<E, false>(in, nv);
+  if constexpr (ANY) {
+    if (d % Rows::kW) kernel = rows_i8_variant<E, true>(in, nv);
+    if (pieces > 4096) kernel = rows_i8_long_kernel<Rows, E>, threads = 1024;
+  }
   launch_timed(PROF_ROWS_I8, kernel, rows, threads, 0, st, in, d, codes, scales, (E*)values);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
+}
+
+int launch_residual_rmsnorm_i8(int dtype, float* x, const float* delta, const I8Sums& sums, const void* gain, float eps, int rows, int d,
+                               int8_t* codes, float* scales, hipStream_t st) {
+  if (sums.n == 0)
+    return medusa_residual_rmsnorm_i8(dtype, x, delta, MDZ_FP32, gain, eps, rows, d, x, codes, scales, nullptr, st);
+  MDZ_REQUIRE(d % 4 == 0 && d <= kI8MaxPartsWidth && sums.n <= kI8MaxParts, MDZ_EUNSUPPORTED, "norm i8: width %d, %d parts", d, sums.n);
+  MDZ_WITH_ELEM16(dtype, return (launch_rows_i8<E, false>(NormOfSumsRows<E>{x, sums, (const E*)gain, d, eps}, rows, d, codes, scales, nullptr, st)));
 }
 
 // One workgroup per row of the padded matrix: codes and scale of a source row, zeros for a row of the padding.
@@ -390,14 +447,14 @@ int medusa_pack_codes_i8(const int8_t* codes, const float* scales, int64_t n_row
 int medusa_quantize_rows_i8(int dtype, const void* src, int rows, int d, int8_t* codes, float* scales, void* values_opt, void* stream) {
   int rc = check_rows_i8("quantize_rows_i8", dtype, src, elem_bytes(dtype), rows, d, codes, scales, values_opt);
   if (rc) return rc;
-  MDZ_WITH_ELEM(dtype, return launch_rows_i8<E>(PlainRows<E>{(const E*)src, d}, rows, d, codes, scales, values_opt, (hipStream_t)stream));
+  MDZ_WITH_ELEM(dtype, return (launch_rows_i8<E, true>(PlainRows<E>{(const E*)src, d}, rows, d, codes, scales, values_opt, (hipStream_t)stream)));
 }
 
 int medusa_swiglu_i8(int dtype, const void* gate_up, int rows, int ffn, int8_t* codes, float* scales, void* values_opt, void* stream) {
   int rc = check_rows_i8("swiglu_i8", dtype, gate_up, elem_bytes(dtype), rows, ffn, codes, scales, values_opt);
   if (rc) return rc;
-  MDZ_WITH_ELEM(dtype, return launch_rows_i8<E>(SwigluRows<E>{(const E*)gate_up, ffn}, rows, ffn, codes, scales, values_opt,
-                                                (hipStream_t)stream));
+  MDZ_WITH_ELEM(dtype, return (launch_rows_i8<E, true>(SwigluRows<E>{(const E*)gate_up, ffn}, rows, ffn, codes, scales, values_opt,
+                                                       (hipStream_t)stream)));
 }
 
 int medusa_residual_rmsnorm_i8(int dtype, const float* x, const void* delta_opt, int delta_dtype, const void* gain, float eps, int rows,
@@ -412,10 +469,10 @@ int medusa_residual_rmsnorm_i8(int dtype, const float* x, const void* delta_opt,
               "residual_rmsnorm_i8: a buffer is not aligned to its elements");
   hipStream_t st = (hipStream_t)stream;
   if (!delta_opt || delta_dtype == MDZ_FP32)
-    MDZ_WITH_ELEM(dtype, return launch_rows_i8<E>(NormRows<E, float>{x, (const float*)delta_opt, (const E*)gain, x_out_opt, d, eps}, rows, d,
-                                                  codes, scales, values_opt, st));
-  MDZ_WITH_ELEM(dtype, return launch_rows_i8<E>(NormRows<E, E>{x, (const E*)delta_opt, (const E*)gain, x_out_opt, d, eps}, rows, d, codes,
-                                                scales, values_opt, st));
+    MDZ_WITH_ELEM(dtype, return (launch_rows_i8<E, true>(NormRows<E, float>{x, (const float*)delta_opt, (const E*)gain, x_out_opt, d, eps},
+                                                         rows, d, codes, scales, values_opt, st)));
+  MDZ_WITH_ELEM(dtype, return (launch_rows_i8<E, true>(NormRows<E, E>{x, (const E*)delta_opt, (const E*)gain, x_out_opt, d, eps}, rows, d,
+                                                     codes, scales, values_opt, st)));
 }
 
 #pragma GCC visibility pop
