@@ -225,7 +225,8 @@ int medusa_swiglu_i8(int dtype, const void* gate_up, int rows, int ffn, int8_t* 
 /* y[m][n] = scales[m] * scale of row n * sum_k codes[m][k] * code[n][k]: codes [M, K], y [M, N] of type out_dtype,
  * packed: an 8-bit [N, K] matrix as above.  The sums are exact in 32-bit integers; a result does not depend on M or on
  * the order of the sums.  ws: medusa_linear_i8_workspace_bytes(M, N, K) bytes of scratch that start on 16
- * bytes (0: ws may be NULL); nothing in it has to be set, and nothing is kept in it. */
+ * bytes (0: ws may be NULL); nothing in it has to be set, and nothing is kept in it.  (Fewer rows can need more bytes: a
+ * workspace for products of several M is as large as the largest of theirs.) */
 int64_t medusa_linear_i8_workspace_bytes(int M, int N, int K);
 int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, int out_dtype,
                      void* y, void* ws, int64_t ws_bytes, void* stream);

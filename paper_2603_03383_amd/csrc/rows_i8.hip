@@ -121,14 +121,14 @@ struct PlainRows {
   __device__ inline void second_reading() {}
 };
 // 1 / (1 + e^-g): the exponential's argument in two parts, so that its rounding does not grow with g; one unit in the last place each for
-// the exponential and the reciprocal
+// the exponential and the reciprocal.  (Where the argument's high part is infinite the low part is not a number; from 2^127 on the
+// sigmoid is below fp32's normal range, and below 2^-127 it is 1.)
 __device__ inline float sigmoid_i8(float g) {
   constexpr float kLog2e = 1.44269504f, kLow = 1.92596303e-8f;  // log2(e) = their sum
   const float hi = -g * kLog2e;
   const float lo = fmaf(-g, kLog2e, -hi) - g * kLow;
   const float e = fast_exp2(hi);
-  // (beyond 2^100 the sigmoid is e^g to the last bit, and far beyond e is infinite, where the correction would make a NaN of it)
-  return __builtin_amdgcn_rcpf(1.f + (hi > 100.f ? e : fmaf(e, lo * 0.693147181f, e)));
+  return __builtin_amdgcn_rcpf(1.f + (fabsf(hi) < 127.f ? fmaf(e, lo * 0.693147181f, e) : e));
 }
 template <typename E>
 struct SwigluRows {

@@ -154,6 +154,21 @@ def test_swiglu(dtype, rows, ffn):
     check_rows(o, o.codes.cpu().numpy(), np.where(bad, np.nan, scales), dtype, 8 + (2.0 ** 24 if small.any() else 0))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_swiglu_of_extreme_gates(dtype):
+    """Gates where the exponential overflows, vanishes or its argument is infinite: the sigmoid is 0 or 1."""
+    big = float(torch.finfo(TD[dtype]).max)
+    gate = torch.tensor([[big, -big, 1e5, -1e5, 90.0, -90.0, 0.0, -0.0], [-big, -1e30, -500.0, -200.0, -1e5, -1e10, -300.0, 0.0]], device=DEV)
+    up = torch.tensor([[1.0, 1.0, -1.0, 1.0, 2.0, 1.0, 5.0, 5.0], [1.0, -1.0, 1.0, 3.0, 1.0, 1.0, 1.0, 7.0]], device=DEV)
+    gu = torch.cat([gate, up], dim=1).to(TD[dtype])
+    o = Out(2, 8, dtype)
+    P.medusa_swiglu_i8(gu, o.codes, o.scales, o.values)
+    assert o.codes.cpu().numpy().tolist() == [[127, 0, 0, 0, 0, 0, 0, 0], [0] * 8]
+    # row 1 holds nothing above 200 e^-200, which fp32 does not have
+    assert abs(float(o.scales[0]) / (float(gu[0, 0]) / 127) - 1) < 2.0 ** -22 and float(o.scales[1]) == 1.0
+    o.check_guard()
+
+
 def make_linear(m, n, k, seed=0, offset=0, full=False):
     """Codes of bell-shaped rows (or extreme ones), the rows starting `offset` bytes behind an aligned address; the packed matrix."""
     g = _gen(seed + m + 3 * n + 7 * k)
@@ -245,6 +260,35 @@ def test_linear_rows_do_not_depend_on_the_batch(n, k):
         y = torch.empty(m, n, device=DEV)
         P.medusa_linear_i8(x[:m], sx[:m], packed, y, workspace(m, n, k))
         assert torch.equal(y, whole[:m]), m
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 codes in a batch's rows, and in a matrix: the last rows are right, from the row kernels through the product."""
+    rows, k, n = 270_000, 16_384, 48
+    src = torch.empty(rows, k, dtype=torch.bfloat16, device=DEV).fill_(1.0)
+    tail = _normal(_gen(1), 5, k, dtype=torch.bfloat16)
+    src[-5:] = tail
+    codes, scales = torch.empty(rows, k, dtype=torch.int8, device=DEV), torch.empty(rows, device=DEV)
+    P.medusa_quantize_rows_i8(src, codes, scales)
+    del src
+    want, want_scales = rows8.quantize_rows(_np(tail))
+    assert np.array_equal(codes[-5:].cpu().numpy(), want) and np.array_equal(_np(scales[-5:]), want_scales)
+    assert bool((codes[:-5] == 127).all())
+    _, _, w, sw, packed = make_linear(1, n, k)
+    y = torch.empty(rows, n, device=DEV)
+    P.medusa_linear_i8(codes, scales, packed, y, workspace(rows, n, k))
+    ref = rows8.linear(want, want_scales, w.cpu().numpy(), sw.cpu().numpy())[1]
+    assert np.abs(_np(y[-5:]) - ref).max() <= 3.001 * 2.0 ** -24 * np.abs(ref).max()
+    assert bool((y[:-5] == y[0]).all())
+    # the same codes as weights: rows of the matrix beyond 2^32
+    packed = torch.empty(P.medusa_packed_i8_bytes(rows, k), dtype=torch.uint8, device=DEV)
+    P.medusa_pack_codes_i8(codes, scales, packed, rows)
+    x, sx = w[:40].contiguous(), sw[:40].contiguous()
+    for m in (3, 40):
+        y = torch.empty(m, rows, device=DEV)
+        P.medusa_linear_i8(x[:m], sx[:m], packed, y, workspace(m, rows, k))
+        assert np.abs(_np(y[:, -5:]) - ref[:, :m].T).max() <= 3.001 * 2.0 ** -24 * np.abs(ref).max()
+        assert bool((y[:, :-5] == y[:, :1]).all())
 
 
 def test_linear_of_rows_without_a_scale():
