@@ -108,14 +108,14 @@ struct I8Plan {
 // 64 bytes, a third slower than the tiles' 128 (us, this kernel / tiles: 24 rows 4096 x 4096 7.0 / 8.9, 32 rows 12288 x 4096 13.1 / 14.2;
 // 22016 x 4096 22.8 / 21.1, 4096 x 11008 16.3 / 14.1).  Beyond, the tile and the number of splits of the least modelled time: the longest
 // of what a CU needs for its workgroups, what the chip needs for all, and W from HBM, which idle CUs slow down; a split adds a launch and
-// its sums' way to memory and back.  Fitted to 2300 timings (1 .. 2048 rows, 688 x 256 .. 22016 x 4096 and 5120 x 13824): what it picks
-// takes 0.8 % longer than the best of them on average, and 13 % at most where a launch takes more than 5 us.
+// its sums' way to memory and back.  Fitted to 4500 timings (17 .. 2048 rows; 688 x 256, 864 x 7968 .. 22016 x 4096 and 5120 x 13824): what it
+// picks takes 0.5 % longer than the best of them on average, and 12 % at most.
 // summed_later: the consumer adds the parts, so a split costs no launch, and has up to kI8MaxParts.
 static I8Plan plan_i8(int M, int N, int K, bool summed_later = false) {
   I8Plan best{-1, 1, 0, 0};
   if (M <= 16 || (M <= 32 && K <= 8192 && (int64_t)N * K <= 1 << 26)) return best;
   const int n_pad = (int)i8_padded_rows(N), stages = (K + 127) / 128, cus = num_cus();
-  const float hbm = (float)N * K * (1e-6f / 5.4f);
+  const float hbm = (float)N * K * (1e-6f / 7.0f);
   float least = 0.f;
   for (int t = 0; t < kNumI8Tiles; ++t) {
     const I8Tile& tile = kI8Tiles[t];
@@ -127,8 +127,8 @@ static I8Plan plan_i8(int M, int N, int K, bool summed_later = false) {
       const float s = (float)((stages + splits - 1) / splits);
       const float rounds = (float)((wgs + cus - 1) / cus);
       const float cu = rounds * s * tile.us_stage * (rounds > 1.f && tile.two ? 0.81f : 1.f);
-      float us = fmaxf(fmaxf(cu, (float)wgs * s * tile.us_all), hbm * sqrtf(rounds * cus / wgs)) + 0.36f * (rounds - 1.f);
-      if (splits > 1) us += (summed_later ? 0.f : 2.f) + (float)splits * M * n_pad * (4e-6f / 2.5f);
+      float us = fmaxf(fmaxf(cu, (float)wgs * s * tile.us_all), hbm * sqrtf(rounds * cus / wgs)) + 0.33f * (rounds - 1.f);
+      if (splits > 1) us += (summed_later ? 0.f : 1.6f) + (float)splits * M * n_pad * (4e-6f / 2.1f);
       if (best.tile < 0 || us < least) best.tile = t, best.splits = splits, least = us;
     }
   }

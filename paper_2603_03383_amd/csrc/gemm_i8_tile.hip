@@ -28,10 +28,13 @@ __global__ void __launch_bounds__(WR * WC * 64) gemm_i8_tile_kernel(I8Product p,
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds_raw[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / WC, wc = wave % WC;
-  // workgroups go round-robin to the 8 XCDs: the row blocks of a column block follow each other on one of them
-  const int xcd = blockIdx.x & 7, seq = blockIdx.x >> 3;
-  const int bn = (seq / nb_m) * 8 + xcd, bm = seq % nb_m;
-  if (bn >= nb_n) return;
+  // Workgroups go round-robin to the 8 XCDs.  Each takes an eighth of the blocks, a column block's row blocks one after the other, so that they
+  // share its weights through the XCD's L2.  (Whole column blocks to each XCD left three of them with 39 workgroups on 32 CUs at 1548 x 2432 x
+  // 1024: 18.5 us, 11.0 so.)
+  const int xcd = blockIdx.x & 7, blocks = nb_m * nb_n;
+  const int block = (int)((int64_t)blocks * xcd >> 3) + (int)(blockIdx.x >> 3);
+  if (block >= (int)((int64_t)blocks * (xcd + 1) >> 3)) return;
+  const int bn = block / nb_m, bm = block % nb_m;
   const int n_stages = (p.K + kI8Stage - 1) / kI8Stage;
   const int lo = (int)((int64_t)blockIdx.z * n_stages / splits), n = (int)((int64_t)(blockIdx.z + 1) * n_stages / splits) - lo;
   const int row0 = bm * XT * 16, tile0 = bn * WT;
@@ -141,7 +144,7 @@ static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream
   const int nb_m = (p.M + WR * MT * 16 - 1) / (WR * MT * 16), nb_n = (p.n_tiles + WC * NT - 1) / (WC * NT);
   auto kernel = gemm_i8_tile_kernel<WR, WC, MT, NT, NS, TO, PARTIAL>;
   MDZ_SET_LDS_ONCE(kernel, kLds);
-  launch_timed(PROF_GEMM_I8, kernel, dim3((unsigned)((nb_n + 7) / 8 * 8) * nb_m, 1, splits), WR * WC * 64, kLds, st, p, partial, nb_m, nb_n, splits);
+  launch_timed(PROF_GEMM_I8, kernel, dim3((unsigned)(((int64_t)nb_m * nb_n + 7) / 8 * 8), 1, splits), WR * WC * 64, kLds, st, p, partial, nb_m, nb_n, splits);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
 }
@@ -149,16 +152,16 @@ static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream
 // Waves (rows x columns of them), 16-row and 16-column tiles of a wave, stages of the ring, and the two times of I8Tile.  Few rows take wide
 // rings of small stages (a CU's intake is the bound, and two workgroups per CU cover each other's start and end); many rows take the
 // largest tiles, which need the fewest bytes per product.
-#define MDZ_I8_TILES(T)         \
-  T(2, 2, 1, 1, 8, .169, .405)  \
-  T(4, 1, 1, 3, 5, .244, .985)  \
-  T(2, 2, 2, 2, 4, .306, .997)  \
-  T(4, 3, 1, 2, 4, .354, 1.58)  \
-  T(2, 4, 3, 1, 5, .369, 1.44)  \
-  T(2, 4, 4, 1, 4, .415, 1.73)  \
-  T(2, 4, 4, 2, 4, .618, 2.54)  \
-  T(4, 4, 4, 2, 3, .948, 3.93)  \
-  T(4, 2, 4, 6, 2, 1.310, 6.08)
+#define MDZ_I8_TILES(T)          \
+  T(2, 2, 1, 1, 8, .137, .421)   \
+  T(4, 1, 1, 3, 5, .265, 1.02)   \
+  T(2, 2, 2, 2, 4, .313, .945)   \
+  T(4, 3, 1, 2, 4, .331, 1.61)   \
+  T(2, 4, 3, 1, 5, .385, 1.49)   \
+  T(2, 4, 4, 1, 4, .426, 1.80)   \
+  T(2, 4, 4, 2, 4, .545, 2.63)   \
+  T(4, 4, 4, 2, 3, .963, 3.82)   \
+  T(4, 2, 4, 6, 2, 1.305, 5.16)
 #define MDZ_I8_TILE_FACTS(WR, WC, MT, NT, NS, STAGE, ALL) \
   {WR * MT * 16, WC * NT * 16, (WR * MT + WC * NT) * 2048 * NS <= 80 * 1024, STAGE##f, ALL##f * 1e-3f},
 const I8Tile kI8Tiles[kNumI8Tiles] = {MDZ_I8_TILES(MDZ_I8_TILE_FACTS)};

@@ -218,12 +218,12 @@ def test_linear(out, m, n, k):
 
 # (tile rows, tile columns, parts of K) that a product of (rows, columns) over about so many features is cut into: every tile, whole and in parts
 PLANS = [((16, 16, 1), (1, 50, 1150)), ((16, 32, 1), (9, 4305, 1150)), ((16, 48, 1), (16, 8355, 1150)), ((32, 16, 1), (17, 30, 1150)),
-         ((32, 32, 1), (33, 47, 1146)), ((32, 32, 4), (33, 17, 2645)), ((32, 48, 1), (17, 8327, 1109)), ((64, 48, 1), (34, 4110, 1121)),
-         ((64, 48, 6), (1352, 16, 3659)), ((64, 64, 1), (65, 6478, 1113)), ((64, 64, 8), (1057, 50, 4004)), ((64, 96, 1), (67, 8235, 1131)),
-         ((64, 96, 8), (66, 1113, 4949)), ((96, 64, 1), (65, 11368, 1147)), ((96, 64, 6), (67, 1832, 3756)), ((128, 64, 1), (97, 12831, 1127)),
-         ((128, 64, 6), (99, 2114, 4477)), ((128, 128, 1), (65, 17990, 1112)), ((128, 128, 4), (66, 5473, 6556)),
-         ((256, 128, 1), (131, 18221, 1136)), ((256, 128, 6), (140, 4113, 7383)), ((256, 192, 1), (263, 21915, 1139)),
-         ((256, 192, 4), (129, 11332, 7474))]
+         ((32, 32, 1), (33, 47, 1146)), ((32, 32, 4), (33, 17, 2645)), ((32, 48, 1), (17, 8327, 1109)), ((64, 48, 1), (33, 8575, 1117)),
+         ((64, 48, 6), (36, 1453, 2968)), ((64, 64, 1), (65, 6478, 1113)), ((64, 64, 8), (35, 1553, 4743)), ((64, 96, 1), (67, 8235, 1131)),
+         ((64, 96, 8), (33, 2082, 4082)), ((96, 64, 1), (65, 11657, 1136)), ((96, 64, 8), (69, 1697, 4932)), ((128, 64, 1), (97, 12831, 1127)),
+         ((128, 64, 6), (2053, 99, 5274)), ((128, 128, 1), (65, 17990, 1112)), ((128, 128, 8), (66, 2739, 7967)),
+         ((256, 128, 1), (131, 18221, 1136)), ((256, 128, 3), (138, 8408, 6439)), ((256, 192, 1), (268, 21467, 1122)),
+         ((256, 192, 2), (130, 18164, 5058))]
 
 
 @pytest.mark.parametrize("plan,shape", PLANS)
