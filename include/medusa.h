@@ -76,7 +76,8 @@ typedef enum { MDZ_KV_PLAIN = 0, MDZ_KV_FP8E4M3 = 1 } mdz_kv_quant;
  * output feature: half the bytes of the weights.  The products' inputs (both norms' outputs, the attention's output, the
  * SwiGLU output) are rounded to 8 bits with one scale per row; gate and up are rounded to the storage dtype before the
  * SwiGLU, everything else is as without it: the residual stream and q, k, v in fp32, the cache, the final norm, the
- * vocabulary matrices and the Medusa heads in the storage dtype. */
+ * vocabulary matrices and the Medusa heads in the storage dtype.  The layers' matrices and the workspace must start on
+ * 16 bytes, gains and x on their elements' size. */
 typedef struct {
   int32_t d, n_heads, head_dim, ffn, vocab, n_layers;
   int32_t dtype; /* mdz_dtype */

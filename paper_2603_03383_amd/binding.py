@@ -301,8 +301,9 @@ def medusa_pack_weight_i8(src: torch.Tensor, dst: torch.Tensor, dst_rows: int, t
 def medusa_pack_codes_i8(codes: torch.Tensor, scales: torch.Tensor, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0,
                          stream=None) -> None:
     """codes int8 [n, k] with scales fp32 [n] -> the same rows of the packed 8-bit matrix dst."""
-    n, k = codes.shape
-    gpu = codes.get_device()
+    if codes.dim() != 2:
+        raise MedusaError(-2, f"codes: {tuple(codes.shape)}, expected rows")
+    (n, k), gpu = codes.shape, codes.get_device()
     _check(lib().medusa_pack_codes_i8(_operand("codes", codes, (n, k), torch.int8, gpu), _operand("scales", scales, (n,), torch.float32, gpu),
                                       n, k, _packed_i8(dst, dst_rows, k, gpu), dst_rows, tile_offset, _stream_of(gpu, stream)))
 

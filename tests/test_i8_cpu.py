@@ -47,7 +47,7 @@ def test_packed_bytes():
         with pytest.raises(P.MedusaError):
             P.medusa_packed_i8_bytes(*bad)
     assert P.medusa_linear_i8_workspace_bytes(0, 5, 7) >= 0
-    for bad in [(-1, 16, 16), (1, 0, 16), (1, 16, 0), (1, 16, 131072)]:
+    for bad in [(-1, 16, 16), (1, 0, 16), (1, 16, 0), (1, 16, 131072), (2 ** 30 + 1, 16, 16), (1, 2 ** 30 + 1, 16), (2 ** 25, 2 ** 15, 16)]:
         with pytest.raises(P.MedusaError):
             P.medusa_linear_i8_workspace_bytes(*bad)
 
@@ -140,7 +140,11 @@ def test_binding_refuses_shapes_and_types():
         lambda: P.medusa_linear_i8(i8(2, 64), f(2), packed, i8(2, 32), stream=0),
         lambda: P.medusa_pack_codes_i8(i8(32, 64), f(31), packed, 32, stream=0),
         lambda: P.medusa_pack_codes_i8(i8(32, 129), f(32), packed, 32, stream=0),
+        lambda: P.medusa_pack_codes_i8(i8(64), f(1), packed, 32, stream=0),
         lambda: P.medusa_pack_weight_i8(i8(32, 64), packed, 32, stream=0),
+        # right in shape and type, but not on a GPU
+        lambda: P.medusa_quantize_rows_i8(h(2, 8), i8(2, 8), f(2), stream=0),
+        lambda: P.medusa_linear_i8(i8(2, 64), f(2), packed, f(2, 32), stream=0),
     ]
     for k, call in enumerate(bad):
         try:
