@@ -143,9 +143,7 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream(stream) -> C.c_void_p:
     if stream is None:
-        # (the handle itself where torch has a call for it: a Stream object takes 3 us to make)
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        stream = torch.cuda.current_stream() if raw is None else raw(torch.cuda.current_device())
+        stream = torch.cuda.current_stream()
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -256,20 +254,25 @@ def _operand(name: str, t: Optional[torch.Tensor], shape, dtype, device: int) ->
     """Address of a tensor that has this shape and type and lies on this GPU; None stays None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape:
-        raise MedusaError(-2, f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
-    if not t.is_contiguous():
-        raise MedusaError(-2, f"{name}: tensors handed to the library must be contiguous")
-    if device < 0 or t.get_device() != device:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape:
+            raise MedusaError(-2, f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+        if not t.is_contiguous():
+            raise MedusaError(-2, f"{name}: tensors handed to the library must be contiguous")
         raise MedusaError(-1, f"{name}: on {t.device}; a call's tensors lie on one GPU")
     return t.data_ptr()
 
 
-def _stream_of(device: int, stream) -> C.c_void_p:
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(device: int, stream):
     """The caller's stream, or the current one, for tensors on this GPU: the library launches on the current device."""
-    if torch.cuda.current_device() != device:
-        raise MedusaError(-1, f"the tensors lie on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream(stream)
+    if device < 0 or torch.cuda.current_device() != device:
+        raise MedusaError(-1, "the tensors do not lie on a GPU" if device < 0 else
+                          f"the tensors lie on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    # (the handle itself where torch has a call for it: a Stream object takes 3 us to make)
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _rows(name: str, t: torch.Tensor):
