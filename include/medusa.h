@@ -186,7 +186,8 @@ int medusa_pack_weight_bf16_as_f16(const void* src, int64_t n_rows, int64_t k, v
  * gets the scale NaN and codes 0 (whatever is computed from it is NaN).  Activations have a scale per row (token),
  * weights one per output feature.  Rows are contiguous and may start anywhere; scales must be 4-byte aligned and
  * 16- and 32-bit elements aligned to their size.  Widths, row counts and numbers of output features are free (0 rows:
- * nothing is enqueued); inputs and outputs must not overlap except where a parameter says so.  */
+ * nothing is enqueued; what would take a launch of 2^32 threads or more is refused); inputs and outputs must not
+ * overlap except where a parameter says so.  */
 
 #define MDZ_I8_TILE_ROWS 16 /* rows per tile of a packed 8-bit matrix */
 

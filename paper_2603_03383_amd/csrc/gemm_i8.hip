@@ -90,6 +90,7 @@ __global__ void __launch_bounds__(NW * 64) gemm_i8_kernel(I8Product p) {
 
 template <int MT, int NT, int NW, int D, typename TO>
 static int launch_narrow(const I8Product& p, hipStream_t st) {
+  MDZ_REQUIRE(i8_launchable((p.n_tiles + NT - 1) / NT, NW * 64), MDZ_EUNSUPPORTED, "linear_i8: %d columns are more than one launch takes", p.N);
   launch_timed(PROF_GEMM_I8, gemm_i8_kernel<MT, NT, NW, D, TO>, dim3((p.n_tiles + NT - 1) / NT, (p.M + MT * 16 - 1) / (MT * 16)), NW * 64, 0, st, p);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
@@ -174,6 +175,7 @@ static int align_rows(I8Product& p, const I8Plan& plan, void* ws, hipStream_t st
   if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.X) % 16 == 0) return MDZ_OK;
   i32x4* aligned = (i32x4*)((char*)ws + plan.aligned_at);
   const int64_t chunks = (int64_t)p.M * (p.kp / 16);
+  MDZ_REQUIRE(i8_launchable((chunks + 255) / 256, 256), MDZ_EUNSUPPORTED, "linear_i8: %d unaligned rows are more than one launch takes", p.M);
   launch_timed(PROF_GEMM_I8, align_rows_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, p.X, p.K, aligned, chunks, (int)(p.kp / 16));
   MDZ_LAUNCH_CHECK();
   p.X = (const int8_t*)aligned, p.ldx = p.kp, p.K = (int)p.kp;

@@ -159,6 +159,8 @@ template <int WR, int WC, int MT, int NT, int NS, typename TO, bool PARTIAL>
 static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream_t st) {
   constexpr int kLds = (WR * MT + WC * NT) * 2048 * NS;
   const int nb_m = (p.M + WR * MT * 16 - 1) / (WR * MT * 16), nb_n = (p.n_tiles + WC * NT - 1) / (WC * NT);
+  MDZ_REQUIRE(i8_launchable(((int64_t)nb_m * nb_n + 7) / 8 * 8, WR * WC * 64), MDZ_EUNSUPPORTED, "linear_i8: %d x %d outputs are more than one launch takes",
+              p.M, p.N);
   auto kernel = gemm_i8_tile_kernel<WR, WC, MT, NT, NS, TO, PARTIAL>;
   MDZ_SET_LDS_ONCE(kernel, kLds);
   launch_timed(PROF_GEMM_I8, kernel, dim3((unsigned)(((int64_t)nb_m * nb_n + 7) / 8 * 8), 1, splits), WR * WC * 64, kLds, st, p, partial, nb_m, nb_n, splits);

@@ -5,6 +5,9 @@
 
 namespace mdz {
 
+// A launch counts its threads in 32 bits.
+inline bool i8_launchable(int64_t workgroups, int threads) { return workgroups * threads <= (int64_t)UINT32_MAX; }
+
 // ---- rows ------------------------------------------------------------------------------------------
 // A row t in 8 bits: scale = max|t| / 127 (1 where that is zero), code = the integer nearest to t / scale, ties to even, clamped to
 // +-127; decided in fp32.  A row that holds a NaN or an infinity has no scale: it becomes NaN and the codes 0, so that everything

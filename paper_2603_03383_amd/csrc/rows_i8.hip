@@ -335,6 +335,7 @@ static int launch_rows_i8(const Rows& in, int rows, int d, int8_t* codes, float*
     if (d % Rows::kW) kernel = rows_i8_variant<E, true>(in, nv);
     if (pieces > 4096) kernel = rows_i8_long_kernel<Rows, E>, threads = 1024;
   }
+  MDZ_REQUIRE(i8_launchable(rows, threads), MDZ_EUNSUPPORTED, "rows i8: %d rows of %d are more than one launch takes", rows, d);
   launch_timed(PROF_ROWS_I8, kernel, rows, threads, 0, st, in, d, codes, scales, (E*)values);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
@@ -380,6 +381,7 @@ static int check_pack_i8(const void* src, int64_t n_rows, int64_t k, const void*
   MDZ_REQUIRE(k <= kI8MaxK && dst_rows <= INT32_MAX - kI8TileRows, MDZ_EUNSUPPORTED,
               "pack i8: [%lld,%lld]: up to %d input features, whose 32-bit sums cannot overflow, and 2^31 rows", (long long)dst_rows,
               (long long)k, kI8MaxK);
+  MDZ_REQUIRE(i8_launchable(i8_padded_rows(n_rows), 256), MDZ_EUNSUPPORTED, "pack i8: %lld rows are more than one launch takes", (long long)n_rows);
   MDZ_REQUIRE((reinterpret_cast<uintptr_t>(dst) & 15) == 0, MDZ_EINVAL, "pack i8: the packed matrix must start on 16 bytes");
   const int64_t end = tile_offset * kI8TileRows + i8_padded_rows(n_rows), all = i8_padded_rows(dst_rows);
   MDZ_REQUIRE(tile_offset <= all / kI8TileRows && end <= all, MDZ_ESHAPE, "pack i8: %lld rows at tile %lld exceed dst_rows %lld",

@@ -112,6 +112,22 @@ def test_refusals_are_status_codes():
     assert lib.medusa_linear_i8(None, None, None, 0, 16, 64, B, None, None, 0, None) == 0
 
 
+def test_more_than_a_launch_takes_is_refused():
+    """A launch has fewer than 2^32 threads, at least 64 of them per row and 256 per 48 columns (few rows), 1024 outputs (tiles) or packed row."""
+    lib, A, B = P.lib(), 4096, P.MDZ_BF16
+    assert [
+        lib.medusa_quantize_rows_i8(B, A, 2 ** 26, 16, A, A, None, None),
+        lib.medusa_swiglu_i8(B, A, 2 ** 30, 16, A, A, None, None),
+        lib.medusa_residual_rmsnorm_i8(B, A, None, 0, A, 1e-5, 2 ** 30, 16, None, A, A, None, None),
+        lib.medusa_pack_weight_i8(B, A, 2 ** 24, 16, A, 2 ** 24, 0, None),
+        lib.medusa_pack_codes_i8(A, A, 2 ** 24, 16, A, 2 ** 24, 0, None),
+        lib.medusa_linear_i8(A, A, A, 1, 2 ** 30, 16, B, A, None, 0, None),
+        lib.medusa_linear_i8(A, A, A, 2 ** 20, 64, 65537, B, A, A, 1 << 60, None),  # rows that have to be aligned first
+        lib.medusa_linear_i8(A, A, A, 40, 2 ** 30, 16, B, A, A, 1 << 60, None),
+    ] == [-3] * 8
+    assert b"launch" in lib.medusa_last_error()
+
+
 def test_binding_refuses_shapes_and_types():
     i8 = lambda *s: torch.zeros(*s, dtype=torch.int8)  # noqa: E731
     f = lambda *s: torch.zeros(*s)  # noqa: E731
