@@ -17,21 +17,25 @@ struct I8Product {
   int M, N, K;
   int64_t ldx, kp;  // kp: padded features of a row of W
   int n_tiles;      // of W
-  bool quads;       // N and Y allow a store of four columns together
 };
 
-// Writes four consecutive columns of a row.  The MFMAs are issued as W x X^T, so a lane holds such a quad.
+// Writes four consecutive columns of a row.  The MFMAs are issued as W x X^T, so a lane holds such a quad; it leaves as one store wherever the row
+// starts.  (An aligned quad beside a store per element is merged with it by the compiler, to three columns and one in fp32, two and two
+// singles in binary16.  us so / unaligned: 1196 x 19319 x 310 binary16 54.4 / 36.8, 781 x 14784 x 1792 fp32 48.0 / 40.2, 200 x 6144 x 4096
+// fp32 15.1 / 14.4; 1024 x 22016 x 4096 bf16, whose quads were whole, 101.6 / 102.3.)
 template <typename TO>
 __device__ inline void store_scaled(const I8Product& p, int row, int col, i32x4 sum, float sx) {
-  struct alignas(sizeof(TO) * 4) Four {
+  struct Four {
     TO v[4];
   };
+  typedef uint32_t Bits __attribute__((ext_vector_type(sizeof(Four) / 4)));
+  typedef Bits Any __attribute__((aligned(1)));
   const float4 sw = *reinterpret_cast<const float4*>(p.sw + col);  // (padded to whole tiles)
   const Four f{{from_float<TO>((float)sum.x * (sx * sw.x)), from_float<TO>((float)sum.y * (sx * sw.y)),
                 from_float<TO>((float)sum.z * (sx * sw.z)), from_float<TO>((float)sum.w * (sx * sw.w))}};
   TO* y = reinterpret_cast<TO*>(p.Y) + (int64_t)row * p.N + col;
-  if (p.quads) {  // (N is a multiple of four: the quad is whole or beyond it)
-    if (col < p.N) *reinterpret_cast<Four*>(y) = f;
+  if (col + 4 <= p.N) {
+    *reinterpret_cast<Any*>(y) = __builtin_bit_cast(Bits, f);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)

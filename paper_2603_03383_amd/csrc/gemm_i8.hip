@@ -162,11 +162,10 @@ static int check_linear_i8(int M, int N, int K) {
   return MDZ_OK;
 }
 
-static I8Product describe(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, void* y, int out_bytes) {
+static I8Product describe(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, void* y) {
   I8Product p{};
   p.X = codes, p.sx = scales, p.W = (const uint8_t*)packed, p.sw = (const float*)((const char*)packed + i8_scales_offset(N, K)), p.Y = y;
   p.M = M, p.N = N, p.K = K, p.ldx = K, p.kp = i8_padded_k(K), p.n_tiles = (int)(i8_padded_rows(N) / kI8TileRows);
-  p.quads = N % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * out_bytes) == 0;
   return p;
 }
 
@@ -190,7 +189,7 @@ int launch_linear_i8_parts(const int8_t* codes, const float* scales, const void*
   const I8Plan plan = plan_i8(M, N, K, true);
   if (plan.splits == 1) return medusa_linear_i8(codes, scales, packed, M, N, K, MDZ_FP32, y, ws, ws_bytes, st);
   MDZ_REQUIRE(ws_bytes >= plan.bytes, MDZ_EWORKSPACE, "linear_i8: workspace %lld < %lld bytes", (long long)ws_bytes, (long long)plan.bytes);
-  I8Product p = describe(codes, scales, packed, M, N, K, y, 4);
+  I8Product p = describe(codes, scales, packed, M, N, K, y);
   int rc = align_rows(p, plan, ws, st);
   if (rc || (rc = launch_i8_tile_parts(p, plan.tile, plan.splits, ws, st))) return rc;
   *sums = I8Sums{(const int32_t*)ws, plan.splits, p.n_tiles * 16, (int64_t)M * p.n_tiles * 16, scales, p.sw};
@@ -234,7 +233,7 @@ int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packe
               (long long)ws_bytes, (long long)plan.bytes);
   MDZ_REQUIRE(plan.bytes == 0 || (reinterpret_cast<uintptr_t>(ws) & 15) == 0, MDZ_EINVAL, "linear_i8: the workspace must start on 16 bytes");
   hipStream_t st = (hipStream_t)stream;
-  I8Product p = describe(codes, scales, packed, M, N, K, y, elem_bytes(out_dtype));
+  I8Product p = describe(codes, scales, packed, M, N, K, y);
   if (plan.tile < 0) MDZ_WITH_ELEM(out_dtype, return (M <= 16 ? launch_few_rows<1, E>(p, st) : launch_few_rows<2, E>(p, st)));
   if ((rc = align_rows(p, plan, ws, st))) return rc;
   return launch_i8_tile(out_dtype, p, plan.tile, plan.splits, ws, st);

@@ -243,6 +243,20 @@ def test_linear_rows_off_alignment(m, n, k, offset):
     check_linear(*make_linear(m, n, k, offset=offset), "fp32")
 
 
+@pytest.mark.parametrize("out", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(1, 61, 128), (5, 64, 100), (24, 47, 256), (33, 17, 2645), (70, 258, 1024), (130, 1003, 256), (300, 769, 512)])
+def test_linear_into_outputs_that_start_anywhere(out, m, n, k):
+    """Four columns leave as one store from any element's address: the same results bit for bit, and nothing around them is written."""
+    x, sx, w, sw, packed = make_linear(m, n, k)
+    want = torch.empty(m, n, dtype=TD[out], device=DEV)
+    P.medusa_linear_i8(x, sx, packed, want, workspace(m, n, k))
+    for first in (1, 2, 3):
+        buf = torch.full((first + m * n + 8,), 7.5, dtype=TD[out], device=DEV)
+        P.medusa_linear_i8(x, sx, packed, buf[first:first + m * n].view(m, n), workspace(m, n, k))
+        assert torch.equal(buf[first:first + m * n].view(m, n), want)
+        assert bool((buf[:first] == 7.5).all()) and bool((buf[first + m * n:] == 7.5).all())
+
+
 @pytest.mark.parametrize("m", [1, 64, 130])
 def test_linear_largest_sum(m):
     """-128 times -128 over the longest row: 2^31 - 16384, the largest sum there can be."""
