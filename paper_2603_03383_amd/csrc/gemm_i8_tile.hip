@@ -14,7 +14,7 @@
 // columns are few: parts of 64 x 64 tiles instead of whole sums of 64 x 16 (64 x 4096 x 11008: 20.6 us whole, 15.4 in four parts with the launch that
 // adds them).  64 x 22016 x 4096: 18.5-21 us as W lies in the memory-side cache or not, 4.3-5 TB/s, against 19.0 at the rate of a large copy.
 // With many rows: 256 x 192 tiles of eight waves, whose loads alone take 50 us per 256 tiles of 4096 features, the LDS reads and MFMAs 47,
-// together 55-62; the matrix cores are 41 % busy and the clock falls with the codes' bits (zeros: 52).  1024 x 22016 x 4096: 100-117 us, 1.6-1.8
+// together 55-62; the matrix cores are 40 % busy and the clock falls with the codes' bits (zeros: 52).  1024 x 22016 x 4096: 100-117 us, 1.6-1.8
 // Pop/s (a library product of the same shape without scales: 133); 1024 x 12288 x 4096: 55 (73); 1024 x 4096 x 11008: 56 (57).
 // Tried and left out: stages of 64 features in deeper rings (half of each cache line of X per load: 5-20 % slower), W non-temporal (+-5 %
 // either way), 256 x 256 tiles (344 of them on 256 CUs: 131 us), one wave per SIMD (155 us), a wave priority around the MFMAs (nothing).
