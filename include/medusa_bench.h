@@ -68,13 +68,25 @@ int medusa_attention_plan(const mdz_model_desc* model, int kv_quant, int B, int 
  * rows nor weights are long) weights go straight to registers: tile_rows is then 16 or 32 and tile_cols 16, 32 or 48.  Needs no device. */
 int medusa_linear_i8_plan(int M, int N, int K, int32_t* tile_rows, int32_t* tile_cols, int32_t* k_splits);
 
-/* ---- test hook --------------------------------------------------------------------------------------- */
+/* The same for a product of a layer whose consumer, a norm that makes codes, adds the parts itself (d = N columns): into how many parts K is split
+ * (1: the product finishes its sums).  Returns the scratch's bytes (negative: mdz_status).  Needs no device. */
+int64_t medusa_linear_i8_parts_plan(int M, int N, int K, int32_t* k_splits);
+
+/* ---- test hooks -------------------------------------------------------------------------------------- */
 
 /* The layer runs RoPE + cache write either fused into the attention kernel's prologue (default) or as a kernel of
  * its own followed by the attention over the rotated queries; both orders are product paths (the second serves the
  * shapes the fused kernel does not cover).  on != 0 forces the second everywhere so that a test can compare them on
  * one shape.  Process-global; returns the previous setting. */
 int medusa_test_force_unfused_rope(int on);
+
+/* A residual update of an 8-bit layer as the layer makes it: x[M, d] += the product of `codes` [M, K] (row scales `scales`) with the packed matrix
+ * [d, K], in parts where the plan above says so, and the next norm of x, whose codes and row scales go to codes_out and scales_out (scales_out may be
+ * scales).  dtype: of gain, bf16 or fp16.  d is a multiple of 32 and at most 16384.  part: [M, d] fp32 of scratch for a product in one part; ws: as the plan
+ * says, on 16 bytes. */
+int medusa_test_i8_update_norm(int dtype, const int8_t* codes, const float* scales, const void* packed, int M, int d, int K, float* x,
+                               const void* gain, float eps, int8_t* codes_out, float* scales_out, float* part, void* ws, int64_t ws_bytes,
+                               void* stream);
 
 #ifdef __cplusplus
 }

@@ -86,6 +86,9 @@ _SIGNATURES = {
     "medusa_swiglu_i8": (C.c_int, [C.c_int, C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 4),
     "medusa_linear_i8_workspace_bytes": (C.c_int64, [C.c_int] * 3),
     "medusa_linear_i8_plan": (C.c_int, [C.c_int] * 3 + [C.c_void_p] * 3),
+    "medusa_linear_i8_parts_plan": (C.c_int64, [C.c_int] * 3 + [C.c_void_p]),
+    "medusa_test_i8_update_norm": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int] * 3 + [C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 4 +
+                                   [C.c_int64, C.c_void_p]),
     "medusa_linear_i8": (C.c_int, [C.c_void_p] * 3 + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "medusa_kv_bytes": (C.c_int64, [C.POINTER(KvDesc)]),
     "medusa_kv_init": (C.c_int, [C.POINTER(KvDesc), C.c_void_p]),
@@ -352,6 +355,24 @@ def medusa_linear_i8_plan(M: int, N: int, K: int) -> dict:
     vals = [C.c_int32() for _ in range(3)]
     _check(lib().medusa_linear_i8_plan(M, N, K, *[C.byref(v) for v in vals]))
     return dict(zip(("tile_rows", "tile_cols", "k_splits"), [v.value for v in vals]))
+
+
+def medusa_linear_i8_parts_plan(M: int, N: int, K: int) -> dict:
+    splits = C.c_int32()
+    need = _check(lib().medusa_linear_i8_parts_plan(M, N, K, C.byref(splits)))
+    return dict(k_splits=splits.value, workspace_bytes=need)
+
+
+def medusa_test_i8_update_norm(codes, scales, packed, x, gain, eps: float, codes_out, scales_out, part, ws, stream=None) -> None:
+    """Test hook (include/medusa_bench.h): x += product, and the next norm's codes and scales, as an 8-bit layer makes them."""
+    (M, d), _, gpu = _rows("x", x)
+    K = codes.shape[-1]
+    _check(lib().medusa_test_i8_update_norm(
+        _STORAGE[gain.dtype], _operand("codes", codes, (M, K), torch.int8, gpu), _operand("scales", scales, (M,), torch.float32, gpu),
+        _packed_i8(packed, d, K, gpu), M, d, K, _operand("x", x, (M, d), torch.float32, gpu), _operand("gain", gain, (d,), gain.dtype, gpu), eps,
+        _operand("codes_out", codes_out, (M, d), torch.int8, gpu), _operand("scales_out", scales_out, (M,), torch.float32, gpu),
+        _operand("part", part, (M, d), torch.float32, gpu), _operand("ws", ws, ws.shape, ws.dtype, gpu), ws.numel() * ws.element_size(),
+        _stream_of(gpu, stream)))
 
 
 def medusa_linear_i8(codes, scales, packed, y, ws=None, stream=None) -> None:

@@ -218,6 +218,29 @@ int medusa_linear_i8_plan(int M, int N, int K, int32_t* tile_rows, int32_t* tile
   return MDZ_OK;
 }
 
+int64_t medusa_linear_i8_parts_plan(int M, int N, int K, int32_t* k_splits) {
+  const int rc = check_linear_i8(M, N, K);
+  if (rc) return rc;
+  if (k_splits) *k_splits = plan_i8(M, N, K, true).splits;
+  const int64_t whole = plan_i8(M, N, K).bytes, parts = linear_i8_parts_bytes(M, N, K);
+  return whole > parts ? whole : parts;
+}
+
+int medusa_test_i8_update_norm(int dtype, const int8_t* codes, const float* scales, const void* packed, int M, int d, int K, float* x,
+                               const void* gain, float eps, int8_t* codes_out, float* scales_out, float* part, void* ws, int64_t ws_bytes,
+                               void* stream) {
+  MDZ_REQUIRE(is_16bit(dtype) && M > 0 && d > 0 && d % 32 == 0 && d <= kI8MaxPartsWidth, MDZ_EINVAL, "i8 update norm: dtype %d, [%d,%d]", dtype, M, d);
+  MDZ_REQUIRE(codes && scales && packed && x && gain && codes_out && scales_out && part && reinterpret_cast<uintptr_t>(ws) % 16 == 0, MDZ_EINVAL,
+              "i8 update norm: bad pointer");
+  const int64_t need = medusa_linear_i8_parts_plan(M, d, K, nullptr);
+  if (need < 0) return (int)need;
+  MDZ_REQUIRE(ws_bytes >= need && (ws || need == 0), MDZ_EWORKSPACE, "i8 update norm: workspace %lld < %lld bytes", (long long)ws_bytes, (long long)need);
+  I8Sums sums{};
+  const int rc = launch_linear_i8_parts(codes, scales, packed, M, d, K, part, ws, ws_bytes, &sums, (hipStream_t)stream);
+  if (rc) return rc;
+  return launch_residual_rmsnorm_i8(dtype, x, part, sums, gain, eps, M, d, codes_out, scales_out, (hipStream_t)stream);
+}
+
 int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, int out_dtype, void* y, void* ws,
                      int64_t ws_bytes, void* stream) {
   MDZ_REQUIRE(dtype_ok(out_dtype), MDZ_EINVAL, "linear_i8: bad dtype %d", out_dtype);

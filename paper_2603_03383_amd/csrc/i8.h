@@ -72,12 +72,12 @@ struct I8Sums {
   const float* sx;
   const float* sw;
 };
-// medusa_linear_i8 into y, or, where that is faster, parts in ws and no second launch; bit for bit the same numbers
+// medusa_linear_i8 into y, or, where that is faster, parts in ws and no second launch, which stand for bit for bit the same numbers
 int launch_linear_i8_parts(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, float* y, void* ws, int64_t ws_bytes,
                            I8Sums* sums, hipStream_t st);
 int64_t linear_i8_parts_bytes(int M, int N, int K);
-// medusa_residual_rmsnorm_i8 in place with such a product as the update (delta where sums.n == 0); parts need d <= kI8MaxPartsWidth and a multiple
-// of four
+// medusa_residual_rmsnorm_i8 in place with such a product as the update (delta where sums.n == 0), the same x and codes bit for bit; parts need
+// d <= kI8MaxPartsWidth and a multiple of four
 constexpr int kI8MaxPartsWidth = 16384;
 int launch_residual_rmsnorm_i8(int dtype, float* x, const float* delta, const I8Sums& sums, const void* gain, float eps, int rows, int d,
                                int8_t* codes, float* scales, hipStream_t st);

@@ -196,7 +196,9 @@ struct NormRows {
   }
 };
 
-// the same with the update still in parts: finished here as the product's own second launch would
+// The same with the update still in parts: finished here as the product's own second launch would.  x' and the codes are bit for bit those of the
+// product and NormRows; the sum of squares is one fused operation per element there where the compiler makes it one, two roundings here, so scales can
+// differ in their last bits.
 template <typename E>
 struct NormOfSumsRows {
   static constexpr int kW = 4;
@@ -224,7 +226,7 @@ struct NormOfSumsRows {
   }
   template <bool TAIL>
   __device__ inline void values(int64_t r, int i, int n, const Raw& raw, float (&t)[kW], float& squares) const {
-#pragma clang fp contract(off)  // every rounding as where the product is stored in between
+#pragma clang fp contract(off)  // every rounding of x' as where the product is stored in between
     i32x4 sum = raw.part[0];
 #pragma unroll
     for (int s = 1; s < kI8MaxParts; ++s)
