@@ -212,7 +212,8 @@ int medusa_quantize_rows_i8(int dtype, const void* src, int rows, int d, int8_t*
 
 /* The residual's addition and RMSNorm with an output in 8 bits: x' = x + delta (fp32), y = x' * gain *
  * rsqrt(mean(x'^2) + eps), codes and scales of the rows of y.  (The codes are those of x' * gain: the factor is
- * positive and goes into the scale alone.)  x [rows, d] fp32; delta_opt (nullable) [rows, d], fp32 or of type dtype, as
+ * positive and goes into the scale alone.  x' * gain and the sum of x'^2 must stay in fp32's range, and with eps = 0 the sum
+ * of a row other than zeros in its normal range.)  x [rows, d] fp32; delta_opt (nullable) [rows, d], fp32 or of type dtype, as
  * delta_dtype says; gain [d] and values_opt of type dtype; x_out_opt (nullable) [rows, d] fp32 receives x' and may be x
  * itself. */
 int medusa_residual_rmsnorm_i8(int dtype, const float* x, const void* delta_opt, int delta_dtype, const void* gain,

@@ -25,15 +25,17 @@ def quantize_rows(t):
 
 
 def rmsnorm_rows(x, delta, gain, eps):
-    """x' = x + delta in fp32; codes of x' * gain; the norm's factor, in 64 bits, goes into the scale (float64)."""
+    """x' = x + delta in fp32; codes of x' * gain; the norm's factor, in 64 bits, goes into the scale (float64), but for a row without a code
+    other than zero, which keeps the scale 1."""
     x = np.asarray(x, dtype=F32)
     if delta is not None:
         x = (x + np.asarray(delta, dtype=F32)).astype(F32)
-    with np.errstate(over="ignore", invalid="ignore"):
+    with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
         codes, s = quantize_rows((x * np.asarray(gain, dtype=F32)).astype(F32))
         x64 = x.astype(np.float64)
         factor = 1.0 / np.sqrt((x64 * x64).mean(axis=-1) + eps)
-    return x, codes, s.astype(np.float64) * factor
+        empty = ~codes.any(axis=-1) & (s == 1)
+        return x, codes, np.where(empty, 1.0, s.astype(np.float64) * factor)
 
 
 def swiglu_rows(gate_up):

@@ -17,14 +17,17 @@ constexpr float kI8Max = 127.f;
 __device__ inline uint32_t abs_bits(float t) { return __float_as_uint(t) & 0x7FFFFFFFu; }
 struct I8Quantiser {
   float scale, inverse;
-  bool bad, plain;  // plain: the quotient below is good; else the division is left to the compiler's sequence for it
+  bool bad, empty, plain;  // plain: the quotient below is good; else the division is left to the compiler's sequence for it
   __device__ explicit I8Quantiser(uint32_t amax_bits) {
     bad = amax_bits >= 0x7F800000u;
     const float s = __uint_as_float(amax_bits) / kI8Max;
-    scale = bad ? __uint_as_float(0x7FC00000u) : s > 0.f ? s : 1.f;
+    empty = s == 0.f;
+    scale = bad ? __uint_as_float(0x7FC00000u) : empty ? 1.f : s;
     inverse = 1.f / scale;
     plain = scale >= 0x1p-100f && scale <= 0x1p100f;
   }
+  // the scale of the row times `factor`: a row of zeros stands for zeros and keeps the scale 1, also where the factor is infinite
+  __device__ inline float scale_times(float factor) const { return empty ? 1.f : scale * factor; }
   __device__ inline float code(float quotient) const { return __builtin_amdgcn_fmed3f(rintf(quotient), -kI8Max, kI8Max); }
   // The codes of W values, as numbers.  Three operations make the rounded quotient: a product with the rounded reciprocal, the rest it
   // leaves, which is exact, and the rest's share (1024 rows of 12800 with SwiGLU: 25.2 us with the

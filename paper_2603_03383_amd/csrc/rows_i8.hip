@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(1024) rows_i8_kernel(Rows in, int d, int8_t* c
   }
   row_statistics(amax, squares);
   const I8Quantiser q(amax);
-  const float scale = q.scale * in.factor(squares);
+  const float scale = q.scale_times(in.factor(squares));
   if (threadIdx.x == 0) scales[r] = scale;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(1024) rows_i8_long_kernel(Rows in, int d, int8
   }
   row_statistics(amax, squares);
   const I8Quantiser q(amax);
-  const float scale = q.scale * in.factor(squares);
+  const float scale = q.scale_times(in.factor(squares));
   if (threadIdx.x == 0) scales[r] = scale;
   in.second_reading();
   for (int i = threadIdx.x * W; i < d; i += 1024 * W) {
