@@ -47,12 +47,17 @@ __device__ inline void store_scaled(const I8Product& p, int row, int col, i32x4 
 // `us_stage`: of one workgroup, us per 128 features; `us_all`: us per 128 features and workgroup where all CUs are busy, which is what the
 // chip's fabric delivers (about 10 TB/s) shared among them; `two`: two workgroups fit a CU's LDS.  See plan_i8.
 struct I8Tile {
-  int rows, cols;
+  int rows, cols, threads;
   bool two;
   float us_stage, us_all;
 };
 constexpr int kNumI8Tiles = 9;
 extern const I8Tile kI8Tiles[kNumI8Tiles];
+// workgroups of one part of the features, as a launch has them: in eights, one for each XCD
+inline int64_t i8_tile_workgroups(const I8Tile& t, int M, int n_tiles) {
+  const int64_t blocks = (int64_t)((M + t.rows - 1) / t.rows) * ((n_tiles * 16 + t.cols - 1) / t.cols);
+  return (blocks + 7) / 8 * 8;
+}
 // The features in `splits` parts: more than one write their 32-bit sums to `partial` (splits x M x 16 n_tiles), and a second launch adds them.
 int launch_i8_tile(int out_dtype, const I8Product& p, int tile, int splits, void* partial, hipStream_t st);
 int launch_i8_tile_parts(const I8Product& p, int tile, int splits, void* partial, hipStream_t st);  // the first launch alone

@@ -169,12 +169,17 @@ static I8Product describe(const int8_t* codes, const float* scales, const void* 
   return p;
 }
 
-// The tiles' loads take 16 bytes from addresses of 16: rows that do not start there go through the workspace.
+// The tiles' loads take 16 bytes from addresses of 16: rows that do not start there go through the workspace.  Both launches' sizes are asked here,
+// before the first of them.  (The parts of a split and the launch that adds them are few: plan_i8 splits up to 4 workgroups per CU.)
 static int align_rows(I8Product& p, const I8Plan& plan, void* ws, hipStream_t st) {
-  if (p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.X) % 16 == 0) return MDZ_OK;
-  i32x4* aligned = (i32x4*)((char*)ws + plan.aligned_at);
+  const bool aligned_already = p.K % 16 == 0 && reinterpret_cast<uintptr_t>(p.X) % 16 == 0;
   const int64_t chunks = (int64_t)p.M * (p.kp / 16);
-  MDZ_REQUIRE(i8_launchable((chunks + 255) / 256, 256), MDZ_EUNSUPPORTED, "linear_i8: %d unaligned rows are more than one launch takes", p.M);
+  MDZ_REQUIRE(i8_launchable(i8_tile_workgroups(kI8Tiles[plan.tile], p.M, p.n_tiles), kI8Tiles[plan.tile].threads), MDZ_EUNSUPPORTED,
+              "linear_i8: %d x %d outputs are more than one launch takes", p.M, p.N);
+  MDZ_REQUIRE(aligned_already || i8_launchable((chunks + 255) / 256, 256), MDZ_EUNSUPPORTED,
+              "linear_i8: %d unaligned rows are more than one launch takes", p.M);
+  if (aligned_already) return MDZ_OK;
+  i32x4* aligned = (i32x4*)((char*)ws + plan.aligned_at);
   launch_timed(PROF_GEMM_I8, align_rows_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, p.X, p.K, aligned, chunks, (int)(p.kp / 16));
   MDZ_LAUNCH_CHECK();
   p.X = (const int8_t*)aligned, p.ldx = p.kp, p.K = (int)p.kp;

@@ -159,8 +159,6 @@ template <int WR, int WC, int MT, int NT, int NS, typename TO, bool PARTIAL>
 static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream_t st) {
   constexpr int kLds = (WR * MT + WC * NT) * 2048 * NS;
   const int nb_m = (p.M + WR * MT * 16 - 1) / (WR * MT * 16), nb_n = (p.n_tiles + WC * NT - 1) / (WC * NT);
-  MDZ_REQUIRE(i8_launchable(((int64_t)nb_m * nb_n + 7) / 8 * 8, WR * WC * 64), MDZ_EUNSUPPORTED, "linear_i8: %d x %d outputs are more than one launch takes",
-              p.M, p.N);
   auto kernel = gemm_i8_tile_kernel<WR, WC, MT, NT, NS, TO, PARTIAL>;
   MDZ_SET_LDS_ONCE(kernel, kLds);
   launch_timed(PROF_GEMM_I8, kernel, dim3((unsigned)(((int64_t)nb_m * nb_n + 7) / 8 * 8), 1, splits), WR * WC * 64, kLds, st, p, partial, nb_m, nb_n, splits);
@@ -182,7 +180,7 @@ static int launch_tile(const I8Product& p, int splits, i32x4* partial, hipStream
   T(4, 4, 4, 2, 3, .963, 3.82)   \
   T(4, 2, 4, 6, 2, 1.305, 5.16)
 #define MDZ_I8_TILE_FACTS(WR, WC, MT, NT, NS, STAGE, ALL) \
-  {WR * MT * 16, WC * NT * 16, (WR * MT + WC * NT) * 2048 * NS <= 80 * 1024, STAGE##f, ALL##f * 1e-3f},
+  {WR * MT * 16, WC * NT * 16, WR * WC * 64, (WR * MT + WC * NT) * 2048 * NS <= 80 * 1024, STAGE##f, ALL##f * 1e-3f},
 const I8Tile kI8Tiles[kNumI8Tiles] = {MDZ_I8_TILES(MDZ_I8_TILE_FACTS)};
 
 template <typename TO, bool PARTIAL>
