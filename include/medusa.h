@@ -226,7 +226,8 @@ int medusa_swiglu_i8(int dtype, const void* gate_up, int rows, int ffn, int8_t* 
                      void* stream);
 
 /* y[m][n] = scales[m] * scale of row n * sum_k codes[m][k] * code[n][k]: codes [M, K], y [M, N] of type out_dtype,
- * packed: an 8-bit [N, K] matrix as above.  The sums are exact in 32-bit integers; a result does not depend on M or on
+ * packed: an 8-bit matrix as above, packed for N rows in total and K features (its scales lie behind its rows, so that fewer columns
+ * than it has cannot be asked for).  The sums are exact in 32-bit integers; a result does not depend on M or on
  * the order of the sums.  ws: medusa_linear_i8_workspace_bytes(M, N, K) bytes of scratch that start on 16
  * bytes (0: ws may be NULL); nothing in it has to be set, and nothing is kept in it.  (Fewer rows can need more bytes: a
  * workspace for products of several M is as large as the largest of theirs.) */

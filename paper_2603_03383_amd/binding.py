@@ -291,9 +291,11 @@ def medusa_packed_i8_bytes(n_rows: int, k: int) -> int:
     return _check(lib().medusa_packed_i8_bytes(n_rows, k))
 
 
-def _packed_i8(dst: torch.Tensor, dst_rows: int, k: int, device: int) -> int:
-    if dst.numel() * dst.element_size() < medusa_packed_i8_bytes(dst_rows, k):
-        raise MedusaError(-2, f"packed: {dst.numel() * dst.element_size()} bytes are too few for [{dst_rows}, {k}]")
+def _packed_i8(dst: torch.Tensor, dst_rows: int, k: int, device: int, whole: bool = False) -> int:
+    """whole: the matrix is read, and its scales stand where its rows end: a buffer of other sizes was packed for another."""
+    got, want = dst.numel() * dst.element_size(), medusa_packed_i8_bytes(dst_rows, k)
+    if got < want or (whole and got != want):
+        raise MedusaError(-2, f"packed: {got} bytes are not those of [{dst_rows}, {k}], {want}")
     return _operand("packed", dst, dst.shape, dst.dtype, device)
 
 
@@ -369,14 +371,15 @@ def medusa_test_i8_update_norm(codes, scales, packed, x, gain, eps: float, codes
     K = codes.shape[-1]
     _check(lib().medusa_test_i8_update_norm(
         _STORAGE[gain.dtype], _operand("codes", codes, (M, K), torch.int8, gpu), _operand("scales", scales, (M,), torch.float32, gpu),
-        _packed_i8(packed, d, K, gpu), M, d, K, _operand("x", x, (M, d), torch.float32, gpu), _operand("gain", gain, (d,), gain.dtype, gpu), eps,
+        _packed_i8(packed, d, K, gpu, whole=True), M, d, K, _operand("x", x, (M, d), torch.float32, gpu), _operand("gain", gain, (d,), gain.dtype, gpu), eps,
         _operand("codes_out", codes_out, (M, d), torch.int8, gpu), _operand("scales_out", scales_out, (M,), torch.float32, gpu),
         _operand("part", part, (M, d), torch.float32, gpu), _operand("ws", ws, ws.shape, ws.dtype, gpu), ws.numel() * ws.element_size(),
         _stream_of(gpu, stream)))
 
 
 def medusa_linear_i8(codes, scales, packed, y, ws=None, stream=None) -> None:
-    """y [M, N] (any storage dtype) = rows (codes [M, K], scales [M]) x the packed 8-bit matrix [N, K], transposed."""
+    """y [M, N] (any storage dtype) = rows (codes [M, K], scales [M]) x the packed 8-bit matrix [N, K], transposed; packed: its
+    medusa_packed_i8_bytes(N, K) bytes."""
     shape, out, gpu = _rows("y", y)
     M, N = shape
     if codes.dim() != 2:
@@ -384,7 +387,7 @@ def medusa_linear_i8(codes, scales, packed, y, ws=None, stream=None) -> None:
     K = codes.shape[1]
     _check(lib().medusa_linear_i8(
         _operand("codes", codes, (M, K), torch.int8, gpu), _operand("scales", scales, (M,), torch.float32, gpu),
-        _packed_i8(packed, N, K, gpu), M, N, K, out, _operand("y", y, shape, y.dtype, gpu),
+        _packed_i8(packed, N, K, gpu, whole=True), M, N, K, out, _operand("y", y, shape, y.dtype, gpu),
         None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu), 0 if ws is None else ws.numel() * ws.element_size(),
         _stream_of(gpu, stream)))
 

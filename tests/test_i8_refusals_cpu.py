@@ -2,6 +2,7 @@
 import os
 
 import pytest
+import torch
 
 import paper_2603_03383_amd as P
 
@@ -20,3 +21,28 @@ def test_a_product_too_large_for_a_launch_is_refused_before_its_rows_are_aligned
     lib, A = P.lib(), 4096
     assert lib.medusa_linear_i8(codes, A, A, 40, 2 ** 30, K, P.MDZ_BF16, A, A, 1 << 60, None) == -3
     assert b"outputs are more than one launch takes" in lib.medusa_last_error()
+
+
+def _i8(*s):
+    return torch.zeros(*s, dtype=torch.int8)
+
+
+def _bf(*s):
+    return torch.zeros(*s, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("n,k", [(16, 64), (32, 128 + 64), (48, 64), (1, 64), (16, 128)])
+def test_a_matrix_packed_for_other_sizes_is_refused(n, k):
+    """A packed matrix ends with its scales: with fewer columns than it has, codes would be read as scales."""
+    packed = torch.zeros(P.medusa_packed_i8_bytes(32, 64), dtype=torch.uint8)
+    with pytest.raises(P.MedusaError) as e:
+        P.medusa_linear_i8(_i8(2, k), torch.zeros(2), packed, torch.zeros(2, n), stream=0)
+    assert e.value.status == -2 and "packed" in str(e.value)
+
+
+@pytest.mark.parametrize("n,k", [(32, 64), (17, 64), (32, 1), (32, 128)])
+def test_a_matrix_of_the_same_padded_sizes_passes_the_check(n, k):
+    packed = torch.zeros(P.medusa_packed_i8_bytes(32, 64), dtype=torch.uint8)
+    with pytest.raises(P.MedusaError) as e:
+        P.medusa_linear_i8(_i8(2, k), torch.zeros(2), packed, torch.zeros(2, n), stream=0)
+    assert e.value.status == -1 and "GPU" in str(e.value)  # what is left to refuse here
