@@ -278,11 +278,19 @@ def _stream_of(device: int, stream):
     return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
 
 
+def _int32(what: str, *sizes: int) -> None:
+    """The library takes these sizes as 32-bit integers (ctypes would hand on their low bits)."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise MedusaError(-3, f"{what}: {sizes}: sizes up to 2^31 - 1")
+
+
 def _rows(name: str, t: torch.Tensor):
     """(shape, storage dtype, GPU) of a tensor of rows."""
     shape, dtype = t.shape, _STORAGE.get(t.dtype)
     if len(shape) != 2 or dtype is None:
         raise MedusaError(-2, f"{name}: {tuple(shape)} {t.dtype}, expected rows of a storage dtype")
+    if (shape[0] | shape[1]) >> 31:
+        _int32(name, *shape)
     return shape, dtype, t.get_device()
 
 
@@ -350,16 +358,19 @@ def medusa_swiglu_i8(gate_up, codes, scales, values=None, stream=None) -> None:
 
 
 def medusa_linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
+    _int32("linear_i8", M, N, K)
     return _check(lib().medusa_linear_i8_workspace_bytes(M, N, K))
 
 
 def medusa_linear_i8_plan(M: int, N: int, K: int) -> dict:
+    _int32("linear_i8", M, N, K)
     vals = [C.c_int32() for _ in range(3)]
     _check(lib().medusa_linear_i8_plan(M, N, K, *[C.byref(v) for v in vals]))
     return dict(zip(("tile_rows", "tile_cols", "k_splits"), [v.value for v in vals]))
 
 
 def medusa_linear_i8_parts_plan(M: int, N: int, K: int) -> dict:
+    _int32("linear_i8", M, N, K)
     splits = C.c_int32()
     need = _check(lib().medusa_linear_i8_parts_plan(M, N, K, C.byref(splits)))
     return dict(k_splits=splits.value, workspace_bytes=need)

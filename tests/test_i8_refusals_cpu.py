@@ -46,3 +46,23 @@ def test_a_matrix_of_the_same_padded_sizes_passes_the_check(n, k):
     with pytest.raises(P.MedusaError) as e:
         P.medusa_linear_i8(_i8(2, k), torch.zeros(2), packed, torch.zeros(2, n), stream=0)
     assert e.value.status == -1 and "GPU" in str(e.value)  # what is left to refuse here
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """The library takes sizes as 32-bit integers; 2^32 + 16 handed on as they are would arrive as 16."""
+    big = 2 ** 32 + 16
+    for sizes in [(big, 16, 16), (1, big, 16), (1, 16, big)]:
+        for query in (P.medusa_linear_i8_workspace_bytes, P.medusa_linear_i8_plan, P.medusa_linear_i8_parts_plan):
+            with pytest.raises(P.MedusaError) as e:
+                query(*sizes)
+            assert e.value.status == -3
+    calls = [  # (no row, or no column, of such a size: nothing has to be allocated)
+        lambda: P.medusa_quantize_rows_i8(_bf(0, big), _i8(0, big), torch.zeros(0), stream=0),
+        lambda: P.medusa_swiglu_i8(_bf(0, big), _i8(0, big // 2), torch.zeros(0), stream=0),
+        lambda: P.medusa_residual_rmsnorm_i8(torch.zeros(0, big), None, _bf(1).expand(big), 1e-5, None, _i8(0, big), torch.zeros(0), stream=0),
+        lambda: P.medusa_linear_i8(_i8(0, 16), torch.zeros(0), _i8(16), torch.zeros(0, big), stream=0),
+    ]
+    for k, call in enumerate(calls):
+        with pytest.raises(P.MedusaError) as e:
+            call()
+        assert e.value.status == -3, (k, e.value)
