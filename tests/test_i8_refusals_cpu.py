@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2603_03383_amd as P
+from paper_2603_03383_amd import binding
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -66,3 +67,89 @@ def test_sizes_beyond_32_bits_are_refused():
         with pytest.raises(P.MedusaError) as e:
             call()
         assert e.value.status == -3, (k, e.value)
+
+
+def _f(*s):
+    return torch.zeros(*s)
+
+
+def _packed():
+    return torch.zeros(P.medusa_packed_i8_bytes(32, 64), dtype=torch.uint8)
+
+
+# Calls whose operands are right but for one; they lie in host memory, which is refused last and with another status, so a check that is missing shows.
+WRONG = {
+    "rows: codes narrower": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 7), _f(2), stream=0),
+    "rows: codes of fp32": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _f(2, 8), _f(2), stream=0),
+    "rows: a scale too many": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 8), _f(3), stream=0),
+    "rows: scales of bf16": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 8), _bf(2), stream=0),
+    "rows: values of another type": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 8), _f(2), _f(2, 8), stream=0),
+    "rows: values of another shape": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 8), _f(2), _bf(2, 9), stream=0),
+    "rows: one axis": lambda: P.medusa_quantize_rows_i8(_bf(8), _i8(8), _f(1), stream=0),
+    "rows: float64": lambda: P.medusa_quantize_rows_i8(torch.zeros(2, 8, dtype=torch.float64), _i8(2, 8), _f(2), stream=0),
+    "rows: transposed": lambda: P.medusa_quantize_rows_i8(_bf(8, 2).t(), _i8(2, 8), _f(2), stream=0),
+    "rows: codes transposed": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(8, 2).t(), _f(2), stream=0),
+    "rows: every other scale": lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 8), _f(4)[::2], stream=0),
+    "norm: x of bf16": lambda: P.medusa_residual_rmsnorm_i8(_bf(2, 8), None, _bf(8), 1e-5, None, _i8(2, 8), _f(2), stream=0),
+    "norm: delta narrower": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), _f(2, 7), _bf(8), 1e-5, None, _i8(2, 8), _f(2), stream=0),
+    "norm: delta of a third type": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), _f(2, 8).half(), _bf(8), 1e-5, None, _i8(2, 8), _f(2), stream=0),
+    "norm: gain shorter": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _bf(7), 1e-5, None, _i8(2, 8), _f(2), stream=0),
+    "norm: gain of integers": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _i8(8), 1e-5, None, _i8(2, 8), _f(2), stream=0),
+    "norm: x_out of bf16": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _bf(8), 1e-5, _bf(2, 8), _i8(2, 8), _f(2), stream=0),
+    "norm: x_out shorter": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _bf(8), 1e-5, _f(1, 8), _i8(2, 8), _f(2), stream=0),
+    "norm: codes wider": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _bf(8), 1e-5, None, _i8(2, 9), _f(2), stream=0),
+    "norm: a scale too few": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _bf(8), 1e-5, None, _i8(2, 8), _f(1), stream=0),
+    "norm: values of fp32": lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), None, _bf(8), 1e-5, None, _i8(2, 8), _f(2), _f(2, 8), stream=0),
+    "swiglu: odd width": lambda: P.medusa_swiglu_i8(_bf(2, 15), _i8(2, 7), _f(2), stream=0),
+    "swiglu: codes as wide as gate and up": lambda: P.medusa_swiglu_i8(_bf(2, 16), _i8(2, 16), _f(2), stream=0),
+    "swiglu: codes in one axis": lambda: P.medusa_swiglu_i8(_bf(2, 16), _i8(16), _f(2), stream=0),
+    "swiglu: scales of fp16": lambda: P.medusa_swiglu_i8(_bf(2, 16), _i8(2, 8), _f(2).half(), stream=0),
+    "swiglu: values of another type": lambda: P.medusa_swiglu_i8(_bf(2, 16), _i8(2, 8), _f(2), _f(2, 8), stream=0),
+    "product: another number of rows": lambda: P.medusa_linear_i8(_i8(2, 64), _f(2), _packed(), _f(3, 32), stream=0),
+    "product: more columns": lambda: P.medusa_linear_i8(_i8(2, 64), _f(2), _packed(), _f(2, 33), stream=0),
+    "product: a scale too few": lambda: P.medusa_linear_i8(_i8(2, 64), _f(1), _packed(), _f(2, 32), stream=0),
+    "product: codes of fp32": lambda: P.medusa_linear_i8(_f(2, 64), _f(2), _packed(), _f(2, 32), stream=0),
+    "product: codes in one axis": lambda: P.medusa_linear_i8(_i8(64), _f(1), _packed(), _f(1, 32), stream=0),
+    "product: y of integers": lambda: P.medusa_linear_i8(_i8(2, 64), _f(2), _packed(), _i8(2, 32), stream=0),
+    "product: y transposed": lambda: P.medusa_linear_i8(_i8(2, 64), _f(2), _packed(), _f(32, 2).t(), stream=0),
+    "product: every other byte of ws": lambda: P.medusa_linear_i8(_i8(2, 64), _f(2), _packed(), _f(2, 32), _i8(64)[::2], stream=0),
+    "pack codes: a scale too few": lambda: P.medusa_pack_codes_i8(_i8(32, 64), _f(31), _packed(), 32, stream=0),
+    "pack codes: more features": lambda: P.medusa_pack_codes_i8(_i8(32, 129), _f(32), _packed(), 32, stream=0),
+    "pack codes: one axis": lambda: P.medusa_pack_codes_i8(_i8(64), _f(1), _packed(), 32, stream=0),
+    "pack codes: codes of uint8": lambda: P.medusa_pack_codes_i8(_packed()[:2048].view(32, 64), _f(32), _packed(), 32, stream=0),
+    "pack weight: integers": lambda: P.medusa_pack_weight_i8(_i8(32, 64), _packed(), 32, stream=0),
+    "pack weight: transposed": lambda: P.medusa_pack_weight_i8(_bf(64, 32).t(), _packed(), 32, stream=0),
+}
+
+
+@pytest.mark.parametrize("what", WRONG)
+def test_a_wrong_operand_is_refused_for_itself(what):
+    with pytest.raises(P.MedusaError) as e:
+        WRONG[what]()
+    assert e.value.status == -2
+
+
+def test_without_the_check_of_operands_these_calls_would_pass(monkeypatch):
+    """What the test above relies on: with a check that looks at nothing (and no GPU to ask for), wrong calls end as right ones do here."""
+    monkeypatch.setattr(binding, "_operand", lambda name, t, *rest: 4096)
+    passed = set()
+    for what, call in WRONG.items():
+        with pytest.raises(P.MedusaError) as e:
+            call()
+        if e.value.status == -1:
+            passed.add(what)
+    kept = {"rows: one axis", "rows: float64", "norm: gain of integers", "product: more columns", "product: codes in one axis", "product: y of integers",
+            "pack codes: more features", "pack codes: one axis", "pack weight: integers"}  # refused before their operands are looked at one by one
+    assert passed == set(WRONG) - kept
+
+
+def test_operands_in_host_memory_are_refused():
+    for call in [lambda: P.medusa_quantize_rows_i8(_bf(2, 8), _i8(2, 8), _f(2), _bf(2, 8), stream=0),
+                 lambda: P.medusa_residual_rmsnorm_i8(_f(2, 8), _f(2, 8), _bf(8), 1e-5, _f(2, 8), _i8(2, 8), _f(2), _bf(2, 8), stream=0),
+                 lambda: P.medusa_swiglu_i8(_bf(2, 16), _i8(2, 8), _f(2), _bf(2, 8), stream=0),
+                 lambda: P.medusa_linear_i8(_i8(2, 64), _f(2), _packed(), _f(2, 32), _i8(64), stream=0),
+                 lambda: P.medusa_pack_codes_i8(_i8(32, 64), _f(32), _packed(), 32, stream=0),
+                 lambda: P.medusa_pack_weight_i8(_bf(32, 64), _packed(), 32, stream=0)]:
+        with pytest.raises(P.MedusaError) as e:
+            call()
+        assert e.value.status == -1 and "GPU" in str(e.value)
