@@ -60,7 +60,8 @@ typedef enum { MDZ_KV_PLAIN = 0, MDZ_KV_FP8E4M3 = 1 } mdz_kv_quant;
 
 #define MDZ_MAX_HEADS 8
 
-/* HOST struct: the decoder's shape. d == n_heads * head_dim (no bias).  n_kv_heads: key/value heads of
+/* HOST struct: the decoder's shape.  It has no size field and its last members came later: build a caller against the header
+ * of the library that it loads.  d == n_heads * head_dim (no bias).  n_kv_heads: key/value heads of
  * grouped-query attention (Table 1 of the paper: 32 query heads, 8 key/value heads); it must divide n_heads, query
  * head h reads key/value head h / (n_heads / n_kv_heads); 0 means n_heads (plain multi-head attention).
  * ffn_f16 = 1 (bf16 models): the two matrix products of every layer's feed-forward block take IEEE binary16
@@ -75,7 +76,8 @@ typedef enum { MDZ_KV_PLAIN = 0, MDZ_KV_FP8E4M3 = 1 } mdz_kv_quant;
  * products" below).  The layers' matrices are then packed by medusa_pack_weight_i8 or medusa_pack_codes_i8, one scale per
  * output feature: half the bytes of the weights.  The products' inputs (both norms' outputs, the attention's output, the
  * SwiGLU output) are rounded to 8 bits with one scale per row; gate and up are rounded to the storage dtype before the
- * SwiGLU, everything else is as without it: the residual stream and q, k, v in fp32, the cache, the final norm, the
+ * SwiGLU (in an fp16 model a gate or up beyond 65504 in magnitude becomes infinite and its row NaN, also where their
+ * product would be smaller), everything else is as without it: the residual stream and q, k, v in fp32, the cache, the final norm, the
  * vocabulary matrices and the Medusa heads in the storage dtype.  The layers' matrices and the workspace must start on
  * 16 bytes, gains and x on their elements' size. */
 typedef struct {

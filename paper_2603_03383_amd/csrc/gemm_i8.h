@@ -44,8 +44,8 @@ __device__ inline void store_scaled(const I8Product& p, int row, int col, i32x4 
 }
 
 // ---- tiles of gemm_i8_tile.hip ---------------------------------------------------------------------
-// `us_stage`: of one workgroup, us per 128 features; `us_all`: us per 128 features and workgroup where all CUs are busy, which is what the
-// chip's fabric delivers (about 10 TB/s) shared among them; `two`: two workgroups fit a CU's LDS.  See plan_i8.
+// `us_stage`: of one workgroup, us per 128 features; `us_all`: us per 128 features and workgroup where all CUs are busy, which is what
+// the chip's fabric and caches deliver shared among them (from 11 TB/s for 256 x 192 tiles to 19 for 32 x 32, whose neighbours share more through the L2); `two`: two workgroups fit a CU's LDS.  See plan_i8.
 struct I8Tile {
   int rows, cols, threads;
   bool two;

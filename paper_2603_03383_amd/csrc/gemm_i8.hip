@@ -114,9 +114,13 @@ struct I8Plan {
 // 64 bytes, a third slower than the tiles' 128 (us, this kernel / tiles: 24 rows 4096 x 4096 7.0 / 8.9, 32 rows 12288 x 4096 13.1 / 14.2;
 // 22016 x 4096 22.8 / 21.1, 4096 x 11008 16.3 / 14.1).  Beyond, the tile and the number of splits of the least modelled time: the longest
 // of what a CU needs for its workgroups, what the chip needs for all, and W from HBM, which idle CUs slow down; a split adds a launch and
-// its sums' way to memory and back.  Fitted to 4500 timings (17 .. 2048 rows; 688 x 256, 864 x 7968 .. 22016 x 4096 and 5120 x 13824): what it
-// picks takes 0.5 % longer than the best of them on average, and 12 % at most.
-// summed_later: the consumer adds the parts, so a split costs no launch, and has up to kI8MaxParts.
+// its sums' way to memory and back.  Fitted to 4500 timings (17 .. 2048 rows; 688 x 256, 864 x 7968 .. 22016 x 4096 and 5120 x 13824) of a build whose
+// outputs left in another way; timed again with the present one, 228 products: what it picks takes 0.7 % longer than the best tile and split on
+// average, 11 % at most (128 x 3696 x 4640).  The rule of up to 32 rows costs 2.9 % on average over 39 products, and up to 31 % where K is short and
+// columns are many (32 x 14624 x 2096: 14.2 us, 10.9 in tiles).  All these K are multiples of 16: the copy of unaligned rows is in no cost.
+// summed_later: the consumer adds the parts, so a split costs no launch, and has up to kI8MaxParts.  Nothing was fitted for it: timed with
+// the norm that follows, 149 products, what it picks takes 1.4 % longer than the best on average, 19 % at most (384 x 5568 x 7008), and 10 % at 64 x 4096 x 4096
+// (whole 12.7 us with the norm, in three parts 11.6).
 static I8Plan plan_i8(int M, int N, int K, bool summed_later = false) {
   I8Plan best{-1, 1, 0, 0};
   if (M <= 16 || (M <= 32 && K <= 8192 && (int64_t)N * K <= 1 << 26)) return best;

@@ -3,15 +3,17 @@
 //   * A workgroup owns a tile of the output.  X and W go straight to an LDS ring (`global_load_lds`, 16 bytes per lane, no registers) in
 //     stages of 128 features: a cache line of each row of X, two k-steps of each tile of W.  One counted wait and one barrier per stage
 //     make a stage everyone's; the stage that all have read is requested anew right behind it.
-//   * The operands of a k-step (v_mfma_i32_16x16x64_i8) are read from LDS while the one before multiplies, across the barrier too (1024 x 22016 x
-//     4096: 120 us without, 117 so; 256 x 128 tiles 139.7 / 130).  The MFMA is issued as W x X^T: a lane ends with four columns of one row.
+//   * The operands of a k-step (v_mfma_i32_16x16x64_i8) are read from LDS while the one before multiplies, across the barrier too (when it
+//     was built in, 1024 x 22016 x 4096 gained 3 %, with 256 x 128 tiles 7 %).  The MFMA is issued as W x X^T: a lane ends with four columns of one row.
 //   * X is row-major; its 16-byte chunks change places by the row's number on the way in, so that the reads take two clocks of the banks per
 //     wave and 256 bytes, which is what they need (no conflicts are counted).  Read to registers in operand order instead, 16 rows x
 //     64 bytes per load, X took three times as long as W's whole kilobytes (64 rows of 4096 x 4096: 13.1 us, 9.5 so; 12288: 17.7, 14.5).
-// What bounds it.  Up to ~300 rows the bytes that the CUs take in, X once per column block and W once per row block: some 40 GB/s per CU with
-// all of them busy, 10 TB/s over the chip, up to 55 GB/s with fewer (64 x 12288 x 4096: 458 KB per CU; 14.9 us, 15.2 without the MFMAs, 13.7
-// with W alone; deeper rings change nothing).  Hence tiles that go by the number of rows, and a split of the features where
-// columns are few: parts of 64 x 64 tiles instead of whole sums of 64 x 16 (64 x 4096 x 11008: 20.6 us whole, 15.4 in four parts with the launch that
+// What bounds it.  Up to 64 rows how W is asked for, not the bytes that a CU can take in: 64 x 12288 x 4096 takes 14.9 us, 15.2 without the MFMAs and 13.7
+// with W alone, which is 197 KB per CU; the kernel of few rows streams the same matrix in 9-10 us over as many workgroups, with up to 72 KB of W
+// in flight per CU over four waves that wait for nobody, where here it is 30 KB behind a barrier per stage.  (Deeper rings changed nothing, so it
+// is not the bytes in flight alone.)  From there to ~300 rows the bytes that the CUs take in, X once per column block and W once per row block:
+// 11 to 19 TB/s over the chip, the smaller tiles more.  Hence tiles that go by the number of rows, and a split of the features where columns are
+// few: parts of 64 x 64 tiles instead of whole sums of 64 x 16 (64 x 4096 x 11008: 20.6 us whole, 15.4 in four parts with the launch that
 // adds them).  64 x 22016 x 4096: 18.5-21 us as W lies in the memory-side cache or not, 4.3-5 TB/s, against 19.0 at the rate of a large copy.
 // With many rows: 256 x 192 tiles of eight waves, whose loads alone take 50 us per 256 tiles of 4096 features, the LDS reads and MFMAs 47,
 // together 55-62; the matrix cores are 40 % busy and the clock falls with the codes' bits (zeros: 52).  1024 x 22016 x 4096: 100-117 us, 1.6-1.8

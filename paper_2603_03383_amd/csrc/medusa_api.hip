@@ -305,8 +305,8 @@ static int run_layer_i8(const mdz_model_desc& m, const mdz_layer_weights& lw, in
     return rc;
   if ((rc = medusa_quantize_rows_i8(m.dtype, att, rows, m.d, codes, scales, nullptr, st))) return rc;
   // Where a norm that makes codes follows, a product may leave its sums in parts for it.  (The norm writes its scales where it reads the
-  // parts' row scales; a row's workgroup has read its own before.)  us per step of 8 layers at 7B widths, prefix 1024: 963 with products that
-  // finish their sums themselves, 935 so.
+  // parts' row scales; a row's workgroup has read its own before.)  us per step of 8 layers at 7B widths, products that finish their sums
+  // themselves / so: 64 nodes at prefix 1024 (down in four parts, O whole) 952 / 934, at 16384 1306 / 1280, three sequences 1474 / 1431.
   I8Sums sums{};
   auto update = [&](const void* packed, int K) {
     if (m.d > kI8MaxPartsWidth) return product(packed, m.d, K, MDZ_FP32, part);
@@ -314,6 +314,8 @@ static int run_layer_i8(const mdz_model_desc& m, const mdz_layer_weights& lw, in
   };
   if ((rc = update(lw.wo, m.d))) return rc;
   if ((rc = launch_residual_rmsnorm_i8(m.dtype, x, part, sums, lw.g_ffn, m.rms_eps, rows, m.d, codes, scales, st))) return rc;
+  // Gate and up leave in the storage type, half the bytes of fp32 out of the product and into the SwiGLU.  Each is off by up to 2^-8 (bf16) or 2^-11
+  // (binary16) of itself; the code that their product becomes is off by up to 2^-8 of the row's largest.
   if ((rc = product(lw.wgateup, 2 * m.ffn, m.d, m.dtype, gu))) return rc;
   if ((rc = medusa_swiglu_i8(m.dtype, gu, rows, m.ffn, codes, scales, nullptr, st))) return rc;
   if (g_next && !xn_next) {

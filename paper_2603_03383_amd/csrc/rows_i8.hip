@@ -3,9 +3,10 @@
 // A row is one workgroup's: its elements are read once, stay in registers while max|t| (and the norm's sum of squares) go around the
 // workgroup in a single exchange, and leave as codes.  The norm needs no second exchange for its factor, because 1 / rms is positive:
 // the codes of x' * gain / rms are those of x' * gain, and the factor goes into the scale.  So the codes do not depend on the order of any sum.
-// What bounds it: up to a row per CU the latency of one load, one exchange and one store (about 4 us as a launch, 64 rows of 4096 like
-// one); beyond, memory: norm 1024 x 5120 (16-bit update, 16-bit values written too) 14.2 us = 4.8 TB/s, 4096 x 8192 78 us = 5.6 TB/s, SwiGLU
-// 1024 x 12800 20.7 us = 4.4 TB/s, 2048 x 11008 33 us = 4.7 TB/s, against 4.9 TB/s of a large copy.
+// What bounds it: up to a row per CU the latency of one load, one exchange and one store (a launch of 4.0-4.8 us, 64 rows of 4096 like
+// one); beyond, memory.  By the stamps of a launch: norm 1024 x 5120 (16-bit update, 16-bit values written too) 13.1 us = 5.2 TB/s, 4096 x 8192
+// 78 us = 5.6 TB/s, SwiGLU 1024 x 12800 20.2 us = 4.5 TB/s, 2048 x 11008 33.5 us = 4.7 TB/s, against 4.9 TB/s of a large copy.  (In a row of
+// calls, where launches overlap at their ends, the first takes 12.4 us a call and the third 16.9.)
 #include "i8.h"
 
 namespace mdz {
@@ -328,7 +329,7 @@ static int launch_rows_i8(const Rows& in, int rows, int d, int8_t* codes, float*
   const int pieces = (d + Rows::kW - 1) / Rows::kW;
   // Up to a row per CU a row's time is the latency of one thread's chain, so a thread takes as little as it can; with more rows, small
   // workgroups leave a CU no idle while one of them starts or ends.  us with up to 1024 / 256 threads before a thread takes more:
-  // SwiGLU 64 x 11008 5.0 / 6.0; norm 1024 x 5120 16.2 / 14.2, 1024 x 4096 14.9 / 12.6, SwiGLU 1024 x 12800 22.2 / 20.9.
+  // SwiGLU 64 x 11008 5.1 / 6.1; norm 1024 x 5120 15.3 / 13.1, 1024 x 4096 13.6 / 11.5, SwiGLU 1024 x 12800 21.9 / 20.2.
   const int most = rows <= num_cus() ? 1024 : 256;
   const int nv = pieces <= most ? 1 : pieces <= 2 * most ? 2 : 4;
   int threads = ((pieces + nv - 1) / nv + 63) / 64 * 64;
