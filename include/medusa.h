@@ -237,6 +237,51 @@ int64_t medusa_linear_i8_workspace_bytes(int M, int N, int K);
 int medusa_linear_i8(const int8_t* codes, const float* scales, const void* packed, int M, int N, int K, int out_dtype,
                      void* y, void* ws, int64_t ws_bytes, void* stream);
 
+/* ---- 4-bit weights -------------------------------------------------------------------------- */
+
+/* Matrices in 4 bits, and products of 16-bit rows with them.  An element of a row is a code q of 0..15; `group` (32, 64 or
+ * 128) consecutive input features of a row share one scale s and one zero point z (0..15; 8 throughout a matrix without
+ * zero points: zeros = 0), and the element stands for (q - z) * s.  The last group of a row may be shorter.  dtype, bf16 or
+ * fp16, is the type of the scales and of the rows that the matrix is multiplied with.  Widths, row counts and numbers of
+ * output features are free (0 rows: nothing is enqueued); rows are contiguous and may start on any element; outputs must
+ * not overlap inputs. */
+
+#define MDZ_I4_TILE_ROWS 16 /* rows per tile of a packed 4-bit matrix */
+
+/* Bytes of a packed 4-bit [n_rows, k] matrix with its scales and, zeros = 1, its zero points (k <= 2^24). */
+int64_t medusa_packed_i4_bytes(int64_t n_rows, int64_t k, int group, int zeros);
+
+/* Quantises a ROW-MAJOR [n_rows, k] matrix of type dtype into rows 16 * tile_offset .. of `dst`, a packed matrix of
+ * dst_rows rows in total that starts on 16 bytes (stacked as for medusa_pack_weight_i8).  zeros = 0: s = max|w| / 7, q = the
+ * integer nearest to w / s, ties to even, plus 8.  zeros = 1: with lo = min(0, least w) and hi = max(0, largest w) of the group,
+ * s = hi / 15 - lo / 15, z = the integer nearest to -lo / s, q = the integer nearest to w / s plus z.  Codes and zero points are
+ * clamped to 0..15; s is rounded to dtype first, everything else is decided in fp32 on the rounded s.  Where s is zero so
+ * is what the group stands for; a group that holds a NaN or an infinity has the scale NaN. */
+int medusa_pack_weight_i4(int dtype, const void* src, int64_t n_rows, int64_t k, int group, int zeros, void* dst,
+                          int64_t dst_rows, int64_t tile_offset, void* stream);
+
+/* The same for a matrix that is in 4 bits already: codes [n_rows, k], one per byte, scales [n_rows, ceil(k / group)] of type
+ * dtype, zeros_opt (nullable: a matrix without zero points) [n_rows, ceil(k / group)].  Of codes and zero points the lower
+ * four bits count. */
+int medusa_pack_codes_i4(int dtype, const uint8_t* codes, const void* scales, const uint8_t* zeros_opt, int64_t n_rows,
+                         int64_t k, int group, void* dst, int64_t dst_rows, int64_t tile_offset, void* stream);
+
+/* y[m][n] = sum_k x[m][k] * w[n][k]: x [M, K] of type dtype, y [M, N] of type out_dtype, packed: a 4-bit matrix of N rows and K
+ * features, packed with this dtype, group and zeros.  Products of a group are summed in fp32, times the scale in fp32, over the
+ * groups in fp32, and rounded once.  A group's sum of 32 |x| must stay in fp32's range (bf16).  A row that holds a NaN or an
+ * infinity gets outputs that are not finite.  ws: medusa_linear_i4_workspace_bytes(M, N, K) bytes of scratch that start on 16
+ * bytes (0: ws may be NULL); nothing in it has to be set, and nothing is kept in it.  (A workspace for products of several
+ * sizes is as large as the largest of theirs.) */
+int64_t medusa_linear_i4_workspace_bytes(int M, int N, int K);
+int medusa_linear_i4(int dtype, const void* x, const void* packed, int M, int N, int K, int group, int zeros, int out_dtype,
+                     void* y, void* ws, int64_t ws_bytes, void* stream);
+
+/* The gated half of a feed-forward block in one launch: y[m][f] = SiLU(sum_k x[m][k] * gate[f][k]) * sum_k x[m][k] * up[f][k],
+ * gate and up two packed 4-bit [ffn, K] matrices, y [M, ffn] of type dtype; both sums and the activation in fp32. */
+int64_t medusa_swiglu_i4_workspace_bytes(int M, int ffn, int K);
+int medusa_swiglu_i4(int dtype, const void* x, const void* gate_packed, const void* up_packed, int M, int ffn, int K, int group,
+                     int zeros, void* y, void* ws, int64_t ws_bytes, void* stream);
+
 /* ---- KV cache ------------------------------------------------------------------------------- */
 
 /* Bytes of EACH of desc->k and desc->v (negative = mdz_status). */

@@ -90,6 +90,13 @@ _SIGNATURES = {
     "medusa_test_i8_update_norm": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int] * 3 + [C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 4 +
                                    [C.c_int64, C.c_void_p]),
     "medusa_linear_i8": (C.c_int, [C.c_void_p] * 3 + [C.c_int] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "medusa_packed_i4_bytes": (C.c_int64, [C.c_int64, C.c_int64, C.c_int, C.c_int]),
+    "medusa_pack_weight_i4": (C.c_int, [C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]),
+    "medusa_pack_codes_i4": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int64, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]),
+    "medusa_linear_i4_workspace_bytes": (C.c_int64, [C.c_int] * 3),
+    "medusa_linear_i4": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p] + [C.c_int] * 6 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "medusa_swiglu_i4_workspace_bytes": (C.c_int64, [C.c_int] * 3),
+    "medusa_swiglu_i4": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int] * 5 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "medusa_kv_bytes": (C.c_int64, [C.POINTER(KvDesc)]),
     "medusa_kv_init": (C.c_int, [C.POINTER(KvDesc), C.c_void_p]),
     "medusa_test_force_unfused_rope": (C.c_int, [C.c_int]),
@@ -401,6 +408,77 @@ def medusa_linear_i8(codes, scales, packed, y, ws=None, stream=None) -> None:
         _packed_i8(packed, N, K, gpu, whole=True), M, N, K, out, _operand("y", y, shape, y.dtype, gpu),
         None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu), 0 if ws is None else ws.numel() * ws.element_size(),
         _stream_of(gpu, stream)))
+
+
+# ---------------------------------------------------------------------------------------------
+# 4-bit weights
+# ---------------------------------------------------------------------------------------------
+MDZ_I4_TILE_ROWS = 16
+
+
+@functools.lru_cache(maxsize=None)
+def medusa_packed_i4_bytes(n_rows: int, k: int, group: int, zeros: bool = False) -> int:
+    return _check(lib().medusa_packed_i4_bytes(n_rows, k, group, int(zeros)))
+
+
+def _packed_i4(name: str, t: torch.Tensor, n: int, k: int, group: int, zeros: bool, device: int) -> int:
+    """Scales and zero points stand where the codes end: a buffer of other sizes was packed for another matrix."""
+    got, want = t.numel() * t.element_size(), medusa_packed_i4_bytes(n, k, group, bool(zeros))
+    if got != want:
+        raise MedusaError(-2, f"{name}: {got} bytes are not those of [{n}, {k}] in groups of {group}, {want}")
+    return _operand(name, t, t.shape, t.dtype, device)
+
+
+def medusa_pack_weight_i4(src: torch.Tensor, group: int, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0, zeros: bool = False, stream=None) -> None:
+    """src [n, k] of bf16 or fp16 -> rows 16 * tile_offset .. of the packed 4-bit matrix dst, quantised in groups of a row's features."""
+    shape, dtype, gpu = _rows("src", src)
+    _check(lib().medusa_pack_weight_i4(dtype, _operand("src", src, shape, src.dtype, gpu), shape[0], shape[1], group, int(zeros),
+                                       _packed_i4("packed", dst, dst_rows, shape[1], group, zeros, gpu), dst_rows, tile_offset, _stream_of(gpu, stream)))
+
+
+def medusa_pack_codes_i4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], group: int, dst: torch.Tensor, dst_rows: int,
+                         tile_offset: int = 0, stream=None) -> None:
+    """codes uint8 [n, k] with scales (bf16 or fp16) and zeros (uint8, or None) [n, ceil(k / group)] -> the same rows of the packed matrix dst."""
+    if codes.dim() != 2 or scales.dtype not in _STORAGE:
+        raise MedusaError(-2, f"codes: {tuple(codes.shape)}, scales: {scales.dtype}, expected rows and scales of a storage dtype")
+    (n, k), gpu = codes.shape, codes.get_device()
+    packed = _packed_i4("packed", dst, dst_rows, k, group, zeros is not None, gpu)
+    groups = (n, -(-k // group))
+    _check(lib().medusa_pack_codes_i4(_STORAGE[scales.dtype], _operand("codes", codes, (n, k), torch.uint8, gpu), _operand("scales", scales, groups, scales.dtype, gpu),
+                                      _operand("zeros", zeros, groups, torch.uint8, gpu), n, k, group, packed, dst_rows, tile_offset, _stream_of(gpu, stream)))
+
+
+def medusa_linear_i4_workspace_bytes(M: int, N: int, K: int) -> int:
+    _int32("linear_i4", M, N, K)
+    return _check(lib().medusa_linear_i4_workspace_bytes(M, N, K))
+
+
+def medusa_swiglu_i4_workspace_bytes(M: int, ffn: int, K: int) -> int:
+    _int32("swiglu_i4", M, ffn, K)
+    return _check(lib().medusa_swiglu_i4_workspace_bytes(M, ffn, K))
+
+
+def medusa_linear_i4(x: torch.Tensor, packed: torch.Tensor, group: int, zeros: bool, y: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y [M, N] (any storage dtype) = x [M, K] (bf16 or fp16) times the packed 4-bit matrix [N, K], transposed."""
+    (M, K), dtype, gpu = _rows("x", x)
+    shape, out, _ = _rows("y", y)
+    N = shape[1]
+    _check(lib().medusa_linear_i4(
+        dtype, _operand("x", x, x.shape, x.dtype, gpu), _packed_i4("packed", packed, N, K, group, zeros, gpu), M, N, K, group, int(zeros), out,
+        _operand("y", y, (M, N), y.dtype, gpu), None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
+
+
+def medusa_swiglu_i4(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, group: int, zeros: bool, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """y [M, ffn] = SiLU(x gate^T) * (x up^T): x [M, K] and y of bf16 or fp16, gate and up packed 4-bit matrices [ffn, K]."""
+    (M, K), dtype, gpu = _rows("x", x)
+    shape, _, _ = _rows("y", y)
+    N = shape[1]
+    _check(lib().medusa_swiglu_i4(
+        dtype, _operand("x", x, x.shape, x.dtype, gpu), _packed_i4("gate", gate, N, K, group, zeros, gpu), _packed_i4("up", up, N, K, group, zeros, gpu),
+        M, N, K, group, int(zeros), _operand("y", y, (M, N), x.dtype, gpu), None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
 
 
 def medusa_kv_bytes(kv: KvDesc) -> int:

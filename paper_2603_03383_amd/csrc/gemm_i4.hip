@@ -1,0 +1,170 @@
+// Matrices in 4 bits: packing, how a product is cut, and the C entries.  The kernel stands in gemm_i4.h.
+#include "i4.h"
+
+namespace mdz {
+
+// ---- packing (once per matrix) -----------------------------------------------------------------------
+// A thread makes one word (eight codes of a row); the thread of a group's first word writes its scale and zero point.  Source: codes, scales and zero
+// points as they are, or (src) a matrix to be quantised, whose group each of its threads goes over.
+struct I4Source {
+  const void* src;
+  const uint8_t* codes;
+  const void* scales;
+  const uint8_t* zeros;
+};
+template <typename E>
+__global__ void __launch_bounds__(256) pack_i4_kernel(I4Source s, int64_t n_rows, int64_t k, int group, bool with_zeros, uint32_t* __restrict__ codes,
+                                                      E* __restrict__ scales, uint8_t* __restrict__ zeros, int64_t blocks, int64_t words) {
+  const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (w >= words) return;
+  const int64_t at = w >> 8, tile = at / blocks, block = at - tile * blocks;
+  const int lane = (int)(w >> 2) & 63, r = lane & 15, in_block = (int)(w & 3) * 32 + (lane >> 4) * 8;
+  const int64_t n = tile * 16 + r, k0 = block * kI4Block + in_block, groups = (k + group - 1) / group, g = k0 / group;
+  float scale = 0.f;
+  int zero = 8, q[8] = {8, 8, 8, 8, 8, 8, 8, 8};
+  if (n < n_rows && g < groups) {
+    if (s.src) {
+      const E* row = reinterpret_cast<const E*>(s.src) + n * k;
+      const int64_t end = min((g + 1) * group, k);
+      float lo = 0.f, hi = 0.f;
+      bool bad = false;
+      for (int64_t i = g * group; i < end; ++i) {
+        const float v = to_float(row[i]);
+        bad |= !(fabsf(v) < INFINITY);
+        lo = fminf(lo, v), hi = fmaxf(hi, v);
+      }
+      // the scale as it will be read: rounded to the storage type
+      scale = to_float(from_float<E>(with_zeros ? hi / 15.f - lo / 15.f : fmaxf(hi, fabsf(lo)) / 7.f));
+      if (bad) {
+        scale = __uint_as_float(0x7FC00000u);
+      } else if (scale > 0.f) {
+        if (with_zeros) zero = (int)fminf(fmaxf(rintf(-lo / scale), 0.f), 15.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          q[e] = k0 + e < k ? (int)fminf(fmaxf(rintf(to_float(row[k0 + e]) / scale) + (float)zero, 0.f), 15.f) : zero;
+      }
+    } else {
+      scale = to_float(reinterpret_cast<const E*>(s.scales)[n * groups + g]);
+      if (with_zeros) zero = s.zeros[n * groups + g] & 15;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[e] = k0 + e < k ? s.codes[n * k + k0 + e] & 15 : zero;
+    }
+  }
+  uint32_t word = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) word |= (uint32_t)q[e] << (4 * i4_field(e));
+  codes[w] = word << 3 | word >> 29;
+  if (in_block % group == 0) {
+    const int64_t to = (at * 16 + r) * (kI4Block / group) + in_block / group;
+    scales[to] = from_float<E>(scale);
+    if (with_zeros) zeros[to] = (uint8_t)zero;
+  }
+}
+
+static int check_sizes_i4(const char* what, int64_t n_rows, int64_t k, int group, int zeros) {
+  MDZ_REQUIRE(n_rows > 0 && k > 0, MDZ_EINVAL, "%s: sizes must be positive", what);
+  MDZ_REQUIRE(i4_group_ok(group) && (zeros == 0 || zeros == 1), MDZ_EINVAL, "%s: groups of 32, 64 or 128 features (%d), zeros 0 or 1 (%d)", what, group, zeros);
+  MDZ_REQUIRE(k <= kI4MaxK && n_rows <= INT32_MAX - kI4TileRows, MDZ_EUNSUPPORTED, "%s: [%lld,%lld]: up to %d input features and 2^31 rows", what,
+              (long long)n_rows, (long long)k, kI4MaxK);
+  return MDZ_OK;
+}
+
+static int pack_i4(int dtype, const I4Source& s, int64_t n_rows, int64_t k, int group, int zeros, void* dst, int64_t dst_rows, int64_t tile_offset,
+                   void* stream) {
+  MDZ_REQUIRE(is_16bit(dtype), dtype_ok(dtype) ? MDZ_EUNSUPPORTED : MDZ_EINVAL, "pack i4: dtype %d: bf16 or fp16", dtype);
+  MDZ_REQUIRE((s.src || (s.codes && s.scales)) && dst, MDZ_EINVAL, "pack i4: NULL pointer");
+  const int rc = check_sizes_i4("pack i4", dst_rows, k, group, zeros);
+  if (rc) return rc;
+  MDZ_REQUIRE(n_rows > 0 && dst_rows >= n_rows && tile_offset >= 0, MDZ_EINVAL, "pack i4: bad sizes");
+  MDZ_REQUIRE((reinterpret_cast<uintptr_t>(dst) & 15) == 0, MDZ_EINVAL, "pack i4: the packed matrix must start on 16 bytes");
+  MDZ_REQUIRE((reinterpret_cast<uintptr_t>(s.src) | reinterpret_cast<uintptr_t>(s.scales)) % 2 == 0, MDZ_EINVAL,
+              "pack i4: a buffer is not aligned to its elements");
+  const int64_t tiles = i4_tiles(n_rows), all = i4_tiles(dst_rows);
+  MDZ_REQUIRE(tile_offset <= all && tile_offset + tiles <= all, MDZ_ESHAPE, "pack i4: %lld rows at tile %lld exceed dst_rows %lld", (long long)n_rows,
+              (long long)tile_offset, (long long)dst_rows);
+  MDZ_REQUIRE(n_rows % kI4TileRows == 0 || tile_offset + tiles == all, MDZ_ESHAPE,
+              "pack i4: n_rows %lld is not a multiple of the tile height %d and this is not the last matrix", (long long)n_rows, kI4TileRows);
+  const int64_t blocks = i4_blocks(k), words = tiles * blocks * 256, first = tile_offset * blocks, groups = kI4Block / group;
+  MDZ_REQUIRE(words <= (int64_t)UINT32_MAX - 255, MDZ_EUNSUPPORTED, "pack i4: [%lld,%lld] is more than one launch takes", (long long)n_rows, (long long)k);
+  char* const to = (char*)dst;
+  hipStream_t st = (hipStream_t)stream;
+  ProfScope prof_(PROF_MISC, st);
+  MDZ_WITH_ELEM16(dtype, (pack_i4_kernel<E><<<(unsigned)((words + 255) / 256), 256, 0, st>>>(
+                             s, n_rows, k, group, zeros != 0, (uint32_t*)(to + first * 1024), (E*)(to + i4_scales_offset(dst_rows, k) + first * 32 * groups),
+                             (uint8_t*)(to + i4_zeros_offset(dst_rows, k, group) + first * 16 * groups), blocks, words)));
+  MDZ_LAUNCH_CHECK();
+  return MDZ_OK;
+}
+
+// ---- products ----------------------------------------------------------------------------------------
+static I4Plan plan_i4(int M, int N, int K, bool gated) { return I4Plan{M <= 16 ? 1 : 4, 2}; }
+
+static int check_product_i4(const char* what, int M, int N, int K) {
+  MDZ_REQUIRE(M >= 0 && N > 0 && K > 0, MDZ_EINVAL, "%s: [%d,%d] x [%d,%d]", what, M, K, N, K);
+  MDZ_REQUIRE(K <= kI4MaxK && M <= 1 << 30 && N <= 1 << 30 && (int64_t)M * N < (int64_t)1 << 40, MDZ_EUNSUPPORTED,
+              "%s: [%d,%d] x [%d,%d]: up to %d input features, 2^30 rows and columns and 2^40 outputs", what, M, K, N, K, kI4MaxK);
+  return MDZ_OK;
+}
+
+static int product_i4(const char* what, int dtype, const void* x, const void* packed, const void* second, int M, int N, int K, int group, int zeros,
+                      int out_dtype, void* y, void* ws, int64_t ws_bytes, void* stream) {
+  MDZ_REQUIRE(is_16bit(dtype), dtype_ok(dtype) ? MDZ_EUNSUPPORTED : MDZ_EINVAL, "%s: dtype %d: bf16 or fp16", what, dtype);
+  MDZ_REQUIRE(dtype_ok(out_dtype), MDZ_EINVAL, "%s: bad dtype %d", what, out_dtype);
+  MDZ_REQUIRE(i4_group_ok(group) && (zeros == 0 || zeros == 1), MDZ_EINVAL, "%s: groups of 32, 64 or 128 features (%d), zeros 0 or 1 (%d)", what, group, zeros);
+  const int rc = check_product_i4(what, M, N, K);
+  if (rc) return rc;
+  if (M == 0) return MDZ_OK;
+  MDZ_REQUIRE(x && packed && y, MDZ_EINVAL, "%s: NULL pointer", what);
+  MDZ_REQUIRE(((reinterpret_cast<uintptr_t>(packed) | reinterpret_cast<uintptr_t>(second)) & 15) == 0, MDZ_EINVAL,
+              "%s: a packed matrix must start on 16 bytes", what);
+  MDZ_REQUIRE(reinterpret_cast<uintptr_t>(x) % 2 == 0 && reinterpret_cast<uintptr_t>(y) % elem_bytes(out_dtype) == 0, MDZ_EINVAL,
+              "%s: a buffer is not aligned to its elements", what);
+  I4Product p{};
+  p.X = x, p.w[0] = i4_matrix(packed, N, K, group), p.w[1] = i4_matrix(second ? second : packed, N, K, group), p.Y = y;
+  p.M = M, p.N = N, p.K = K, p.out_dtype = out_dtype, p.n_tiles = (int)i4_tiles(N), p.n_blocks = (int)i4_blocks(K);
+  const I4Plan plan = plan_i4(M, N, K, second != nullptr);
+  hipStream_t st = (hipStream_t)stream;
+  const bool z = zeros != 0, gated = second != nullptr;
+  MDZ_WITH_ELEM16(dtype, return (group == 128 ? launch_i4<E, 1>(p, z, gated, plan, st) : group == 64 ? launch_i4<E, 2>(p, z, gated, plan, st)
+                                                                                                  : launch_i4<E, 4>(p, z, gated, plan, st)));
+}
+
+}  // namespace mdz
+
+using namespace mdz;
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+int64_t medusa_packed_i4_bytes(int64_t n_rows, int64_t k, int group, int zeros) {
+  const int rc = check_sizes_i4("packed_i4_bytes", n_rows, k, group, zeros);
+  return rc ? rc : i4_packed_bytes(n_rows, k, group, zeros != 0);
+}
+
+int medusa_pack_weight_i4(int dtype, const void* src, int64_t n_rows, int64_t k, int group, int zeros, void* dst, int64_t dst_rows, int64_t tile_offset,
+                          void* stream) {
+  return pack_i4(dtype, I4Source{src, nullptr, nullptr, nullptr}, n_rows, k, group, zeros, dst, dst_rows, tile_offset, stream);
+}
+
+int medusa_pack_codes_i4(int dtype, const uint8_t* codes, const void* scales, const uint8_t* zeros_opt, int64_t n_rows, int64_t k, int group, void* dst,
+                         int64_t dst_rows, int64_t tile_offset, void* stream) {
+  return pack_i4(dtype, I4Source{nullptr, codes, scales, zeros_opt}, n_rows, k, group, zeros_opt != nullptr, dst, dst_rows, tile_offset, stream);
+}
+
+int64_t medusa_linear_i4_workspace_bytes(int M, int N, int K) { return check_product_i4("linear_i4", M, N, K); }
+
+int64_t medusa_swiglu_i4_workspace_bytes(int M, int ffn, int K) { return check_product_i4("swiglu_i4", M, ffn, K); }
+
+int medusa_linear_i4(int dtype, const void* x, const void* packed, int M, int N, int K, int group, int zeros, int out_dtype, void* y, void* ws,
+                     int64_t ws_bytes, void* stream) {
+  return product_i4("linear_i4", dtype, x, packed, nullptr, M, N, K, group, zeros, out_dtype, y, ws, ws_bytes, stream);
+}
+
+int medusa_swiglu_i4(int dtype, const void* x, const void* gate_packed, const void* up_packed, int M, int ffn, int K, int group, int zeros, void* y, void* ws,
+                     int64_t ws_bytes, void* stream) {
+  MDZ_REQUIRE(gate_packed && up_packed, MDZ_EINVAL, "swiglu_i4: NULL pointer");
+  return product_i4("swiglu_i4", dtype, x, gate_packed, up_packed, M, ffn, K, group, zeros, dtype, y, ws, ws_bytes, stream);
+}
+
+#pragma GCC visibility pop
+}  // extern "C"

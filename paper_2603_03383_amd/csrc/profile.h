@@ -18,6 +18,7 @@ enum ProfTag {
   PROF_GEMM_N32,     // gemm_mfma_kernel<2,1,1,*>: <= 32 rows (development plans only)
   PROF_GEMM_LARGE,   // gemm_tile_kernel, gemm_wide_kernel: more than 64 rows (several sequences)
   PROF_GEMM_I8,      // product of 8-bit rows with 8-bit weights
+  PROF_GEMM_I4,      // products with 4-bit weights
   PROF_ATTN,         // tree-masked attention (+ its combine pass)
   PROF_NORM,         // RMSNorm
   PROF_ROWS_I8,      // rows in 8 bits: norm, SwiGLU, plain
