@@ -7,46 +7,41 @@ namespace mdz {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-// Codes to 16-bit operands.  A field of four bits under a fixed exponent is a number with the code in its mantissa: 16 + q in bf16, 128 + q in
-// binary16, both exact.  binary16 has a packed addition, which takes 128 + z off and leaves q - z, exact too.  bf16 has none: its products are
-// made with 16 + q and the sum of x over the group, times 16 + z, is taken off them in fp32 (kOffset below): the sums are some six times
-// larger than with q - z and lose that much in their last bits, 2^-24 relative to them.
+// Codes to 16-bit operands.  A field of four bits at the top of a mantissa, under the exponent of 16, is 16 + q: one mask and one exponent make two
+// operands of a word.  The products are made with 16 + q; what is too much, (16 + z) times the sum of x over the group, is taken off in fp32.  The sums
+// are then some six times larger than with q - z and lose that much in their last bits, 2^-24 relative to them.  (binary16 has a packed
+// subtraction that makes q - z of it, 16 more instructions per tile and block; bf16 has none.)
+// The mask and the exponent are kept from the compiler as constants: from registers (w & mask) | magic is one instruction, from literals two.  (No
+// inline assembly for it: the wait between a vector instruction and the MFMA that reads its result is the compiler's to see.)
+constexpr float kI4Offset = 16.f;
 template <typename E>
 struct I4Elem;
 template <>
 struct I4Elem<bf16_t> {
-  static constexpr uint32_t kMagic = 0x41804180u;
-  static constexpr float kOffset = 16.f;  // left on each code
-  static constexpr bool kSums = true;     // the products need the sums of x
   typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+  static constexpr uint32_t kMask = 0x00780078u, kMagic = 0x41804180u, kOne = 0x3F803F80u, kMinus24 = 0xC1C0C1C0u;
   __device__ static inline f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
-  __device__ static inline uint32_t minus(uint32_t w, uint32_t) { return w; }
-  __device__ static inline uint32_t zero_pair(int) { return 0; }
 };
 template <>
 struct I4Elem<f16_t> {
-  static constexpr uint32_t kMagic = 0x58005800u;
-  static constexpr float kOffset = 0.f;
-  static constexpr bool kSums = false;
   typedef _Float16 v8 __attribute__((ext_vector_type(8)));
-  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kMask = 0x03C003C0u, kMagic = 0x4C004C00u, kOne = 0x3C003C00u, kMinus24 = 0xCE00CE00u;
   __device__ static inline f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
-  __device__ static inline uint32_t minus(uint32_t w, uint32_t zp) {
-    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, w) - __builtin_bit_cast(h2, zp));
-  }
-  __device__ static inline uint32_t zero_pair(int z) { return (0x5800u | (uint32_t)z << 3) * 0x00010001u; }  // 128 + z twice
 };
-
 template <typename E>
-__device__ inline u32x4_t dequantise(uint32_t w, uint32_t zp) {
-  constexpr uint32_t kMask = 0x00780078u, kMagic = I4Elem<E>::kMagic;
-  const uint32_t r[4] = {(w & kMask) | kMagic, (w >> 4 & kMask) | kMagic, (w >> 8 & kMask) | kMagic,
-                         (__builtin_amdgcn_alignbit(w, w, 12) & kMask) | kMagic};
-  return u32x4_t{I4Elem<E>::minus(r[0], zp), I4Elem<E>::minus(r[1], zp), I4Elem<E>::minus(r[2], zp), I4Elem<E>::minus(r[3], zp)};
+struct I4Constants {
+  uint32_t mask = I4Elem<E>::kMask, magic = I4Elem<E>::kMagic;
+  __device__ inline I4Constants() { asm volatile("" : "+s"(mask), "+v"(magic)); }
+};
+// features 2 i and 2 i + 1 of a word stand 4 i bits above the mask (i4_rotation)
+template <typename E>
+__device__ inline u32x4_t dequantise(uint32_t w, const I4Constants<E>& c) {
+  return u32x4_t{(w & c.mask) | c.magic, (w >> 4 & c.mask) | c.magic, (__builtin_amdgcn_alignbit(w, w, 8) & c.mask) | c.magic,
+                 (__builtin_amdgcn_alignbit(w, w, 12) & c.mask) | c.magic};
 }
 
 template <typename E>
@@ -70,96 +65,199 @@ __device__ inline void store_four(T* y, int left, f32x4_t v) {
   }
 }
 
+// of a block: scales of four rows, and their zero points
+template <int G>
+struct I4Scales {
+  uint32_t w[2 * G];
+};
+template <int G>
+struct I4Zeros {
+  uint32_t w[G];
+};
+// uniform bases of a wave's tiles, and a lane's place in a block
+template <int G, bool ZEROS, bool GATED, int NT>
+struct I4Stream {
+  static constexpr int kGateTiles = GATED ? NT / 2 : NT;
+  const uint8_t* codes[NT];
+  const uint8_t* scales[NT];
+  const uint8_t* zeros[NT];
+  uint32_t co, so, zo;
+  __device__ inline I4Stream(const I4Product& p, int tile0, int lane) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const I4Matrix& w = p.w[j >= kGateTiles];
+      const int64_t at = (int64_t)min(tile0 + j % kGateTiles, p.n_tiles - 1) * p.n_blocks;
+      codes[j] = w.codes + at * 1024;
+      scales[j] = w.scales + at * (32 * G);
+      zeros[j] = ZEROS ? w.zeros + at * (16 * G) : nullptr;
+    }
+    co = lane * 16, so = (lane >> 4) * (8 * G), zo = (lane >> 4) * (4 * G);
+  }
+  __device__ inline void load(u32x4_t (&c)[NT], I4Scales<G> (&s)[NT], I4Zeros<G> (&z)[NT], int b) const {
+    const int64_t at = __builtin_amdgcn_readfirstlane(b);
+    // A block's address is uniform and a lane's place in it 32 bits (kept from the compiler, which would make 64-bit vector addresses of them).
+    uint32_t c0 = co, s0 = so, z0 = zo;
+    asm volatile("" : "+v"(c0), "+v"(s0), "+v"(z0));
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const u32x4_t* const cp = reinterpret_cast<const u32x4_t*>(codes[j] + at * 1024 + c0);
+      c[j] = __builtin_nontemporal_load(cp);
+      s[j] = *reinterpret_cast<const I4Scales<G>*>(scales[j] + at * (32 * G) + s0);
+      if constexpr (ZEROS) {
+        z[j] = *reinterpret_cast<const I4Zeros<G>*>(zeros[j] + at * (16 * G) + z0);
+      }
+    }
+  }
+};
+
+// What the products with 16 + q have too much, by the matrix cores: -24 times the sums of x over the groups, which the sums of a matrix without zero
+// points start from, or the sums themselves.  x[s][i]: the operands of a block's four steps.
+template <typename E, int G, bool ZEROS, int MT>
+__device__ inline void sum_block(f32x4_t (&c0)[G][MT], const u32x4_t (&x)[4][MT]) {
+  constexpr uint32_t kFactor = ZEROS ? I4Elem<E>::kOne : I4Elem<E>::kMinus24;
+  const u32x4_t factor{kFactor, kFactor, kFactor, kFactor};
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      f32x4_t a{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = g * (4 / G); s < (g + 1) * (4 / G); ++s) a = I4Elem<E>::mfma(factor, x[s][i], a);
+      c0[g][i] = a;
+    }
+}
+
+// tot += the products of one block of features and one tile of columns
+template <typename E, int G, bool ZEROS, int MT>
+__device__ inline void multiply_tile(f32x4_t (&tot)[MT], const u32x4_t (&x)[4][MT], const f32x4_t (&c0)[G][MT], u32x4_t codes, const I4Scales<G>& scales,
+                                     const I4Zeros<G>& zeros, const I4Constants<E>& constants) {
+  constexpr int kSteps = 4 / G;  // MFMA steps of a group
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    f32x4_t acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = ZEROS ? f32x4_t{0.f, 0.f, 0.f, 0.f} : c0[g][i];
+#pragma unroll
+    for (int s = g * kSteps; s < (g + 1) * kSteps; ++s) {
+      const uint32_t word = codes[s];
+      const u32x4_t w = dequantise<E>(word, constants);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[i] = I4Elem<E>::mfma(w, x[s][i], acc[i]);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int at = c * G + g;
+      const float scale = half_to_float<E>(scales.w[at >> 1], at & 1);
+      const float off = ZEROS ? -kI4Offset - (float)(zeros.w[at >> 2] >> (8 * (at & 3)) & 0xFFu) : 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) tot[i][c] = fmaf(scale, ZEROS ? fmaf(off, c0[g][i].x, acc[i][c]) : acc[i][c], tot[i][c]);
+    }
+  }
+}
+
+// Sums over WK waves that made the same outputs of their parts of the features, the activation, and the way out.  A workgroup's waves are WN groups of columns x
+// WK parts; `red`: LDS of WN x WK x MT x NT KiB.
+template <typename E, bool GATED, int MT, int NT, int WN, int WK>
+__device__ inline void finish_i4(const I4Product& p, const f32x4_t (&tot)[NT][MT], f32x4_t* red, int row0, int tile0, int wn, int wk, int lane) {
+  constexpr int kTiles = MT * NT, kGateTiles = GATED ? NT / 2 : NT;
+  auto put = [&](int i, int j, f32x4_t v, f32x4_t up) {
+    if constexpr (GATED) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = silu_tile(v[c]) * up[c];
+    }
+    const int row = row0 + i * 16 + (lane & 15), col = (tile0 + j) * 16 + 4 * (lane >> 4);
+    if (row >= p.M || col >= p.N) return;
+    const int64_t at = (int64_t)row * p.N + col;
+    if (!GATED && p.out_dtype == MDZ_FP32) store_four(reinterpret_cast<float*>(p.Y) + at, p.N - col, v);
+    else if (!GATED && p.out_dtype != (__is_same(E, bf16_t) ? MDZ_BF16 : MDZ_FP16))
+      store_four(reinterpret_cast<std::conditional_t<__is_same(E, bf16_t), f16_t, bf16_t>*>(p.Y) + at, p.N - col, v);
+    else store_four(reinterpret_cast<E*>(p.Y) + at, p.N - col, v);
+  };
+  if constexpr (WK == 1) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < kGateTiles; ++j) put(i, j, tot[j][i], tot[GATED ? kGateTiles + j : j][i]);
+  } else {
+    __syncthreads();
+    f32x4_t* const mine = red + wn * WK * kTiles * 64;  // [part][tile][lane]
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) mine[(wk * kTiles + t) * 64 + lane] = tot[t % NT][t / NT];
+    __syncthreads();
+    auto sum = [&](int tile) {
+      f32x4_t v = mine[tile * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < WK; ++w) v += mine[(w * kTiles + tile) * 64 + lane];
+      return v;
+    };
+    for (int t = wk; t < MT * kGateTiles; t += WK) {
+      const int i = t / kGateTiles, j = t % kGateTiles;
+      put(i, j, sum(i * NT + j), GATED ? sum(i * NT + kGateTiles + j) : f32x4_t{});
+    }
+  }
+}
+
 // A workgroup of NW waves makes 16 MT rows x NT tiles of 16 columns (GATED: NT / 2 of each matrix); the waves share out the blocks of
 // features, so each streams contiguous weights, and their sums meet in LDS.  A wave's rows of X pass through LDS of its own, which turns whole
 // lines of memory into operands; no wave waits for another before the end.  XR: pieces of four rows that are loaded (4 MT, or fewer).
-template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D>
-__global__ void __launch_bounds__(NW * 64) gemm_i4_kernel(I4Product p) {
-  typedef I4Elem<E> El;
-  constexpr int kTiles = MT * NT, kGateTiles = GATED ? NT / 2 : NT;
-  constexpr int kSteps = 4 / G;  // MFMA steps of a group
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D, int DX, int WPE>
+__global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
+  typedef I4Stream<G, ZEROS, GATED, NT> Stream;
   typedef u32x4_t Any16 __attribute__((aligned(1)));
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds_raw[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q4 = lane >> 4, r16 = lane & 15;
-  // Workgroups go round-robin to the 8 XCDs: each takes an eighth of the blocks, a column block's row blocks one after the other.
-  const int xcd = blockIdx.x & 7, blocks = p.nb_m * p.nb_n;
-  const int block = (int)((int64_t)blocks * xcd >> 3) + (int)(blockIdx.x >> 3);
-  if (block >= (int)((int64_t)blocks * (xcd + 1) >> 3)) return;
-  const int row0 = block % p.nb_m * MT * 16, tile0 = block / p.nb_m * kGateTiles;
+  const int row0 = blockIdx.y * MT * 16, tile0 = blockIdx.x * Stream::kGateTiles;
   const int lo = (int)((int64_t)wave * p.n_blocks / NW), hi = (int)((int64_t)(wave + 1) * p.n_blocks / NW);
   const int last_row = p.M - 1 - row0;
-
-  const uint16_t* const x0 = reinterpret_cast<const uint16_t*>(p.X) + (int64_t)row0 * p.K;
-  const uint8_t* cp[NT];
-  const uint8_t* sp[NT];
-  const uint8_t* zp[NT];
+  const uint8_t* const x0 = reinterpret_cast<const uint8_t*>(p.X) + (int64_t)row0 * p.K * 2;
+  const Stream stream(p, tile0, lane);
+  u32x4_t xb[DX][XR], cb[D][NT];
+  I4Scales<G> sb[D][NT];
+  I4Zeros<G> zb[D][NT];
+  uint32_t xo[XR];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const I4Matrix& w = p.w[j >= kGateTiles];
-    const int64_t at = (int64_t)min(tile0 + j % kGateTiles, p.n_tiles - 1) * p.n_blocks;
-    cp[j] = w.codes + at * 1024 + lane * 16;
-    sp[j] = w.scales + at * (32 * G) + q4 * (8 * G);
-    zp[j] = ZEROS ? w.zeros + at * (16 * G) + (El::kSums ? q4 * (4 * G) : r16 * G) : nullptr;
-  }
-  // what a wave has requested of a block: X in pieces of 4 rows x 256 bytes, codes, scales, zero points
-  constexpr int kScaleWords = 2 * G, kZeroWords = El::kSums ? G : 1;
-  struct Scales {
-    uint32_t w[kScaleWords];
-  };
-  struct Zeros {
-    uint32_t w[kZeroWords];
-  };
-  u32x4_t xb[XR], cb[D][NT];
-  Scales sb[D][NT];
-  Zeros zb[D][NT];
-  auto load_x = [&](int b) {
-    const int k = min(b, hi - 1) * kI4Block + r16 * 8;
+  for (int i = 0; i < XR; ++i) xo[i] = (uint32_t)min(i * 4 + q4, last_row) * (uint32_t)(2 * p.K) + r16 * 16;
+  const int whole = p.K / kI4Block, end = min(hi, whole);  // whole blocks of features, and this wave's
+  auto load_x = [&](int slot, int b) {
+    const uint8_t* const at = x0 + (int64_t)__builtin_amdgcn_readfirstlane(min(b, end - 1)) * (2 * kI4Block);
 #pragma unroll
     for (int i = 0; i < XR; ++i) {
-      const uint16_t* row = x0 + (int64_t)min(i * 4 + q4, last_row) * p.K;
-      if (k + 8 <= p.K) {
-        xb[i] = *reinterpret_cast<const Any16*>(row + k);
-      } else {  // the features behind the last: zeros
-        uint32_t v[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (k + e < p.K) v[e >> 1] |= (uint32_t)row[k + e] << 16 * (e & 1);
-        xb[i] = u32x4_t{v[0], v[1], v[2], v[3]};
-      }
-    }
-  };
-  auto load_w = [&](int slot, int b) {
-    const int64_t at = min(b, hi - 1);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      cb[slot][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(cp[j] + at * 1024));
-      sb[slot][j] = *reinterpret_cast<const Scales*>(sp[j] + at * (32 * G));
-      if constexpr (ZEROS) {
-        const uint8_t* z = zp[j] + at * (16 * G);
-        if constexpr (El::kSums) zb[slot][j] = *reinterpret_cast<const Zeros*>(z);
-        else zb[slot][j].w[0] = G == 1 ? *z : G == 2 ? *reinterpret_cast<const uint16_t*>(z) : *reinterpret_cast<const uint32_t*>(z);
-      }
+      uint32_t o = xo[i];
+      asm volatile("" : "+v"(o));
+      xb[slot][i] = *reinterpret_cast<const Any16*>(at + o);
     }
   };
   uint8_t* const xs = lds_raw + wave * (XR * 1024);
 
-  f32x4_t tot[MT][NT];
+  f32x4_t tot[NT][MT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
+  for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) tot[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < MT; ++i) tot[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  auto block_of_features = [&](int slot, int next_x) {
-    // 16-byte chunk c of a row stands at place c ^ (row % 16) of its 256 bytes, so that 16 rows' chunks are read without bank conflicts
+  // the rows' block to LDS: 16-byte chunk c of a row stands at place c ^ (row % 16) of its 256 bytes, so that 16 rows' chunks are read without
+  // bank conflicts
+  auto put_x = [&](int slot) {
 #pragma unroll
     for (int i = 0; i < XR; ++i) {
       const int row = i * 4 + q4;
-      *reinterpret_cast<u32x4_t*>(xs + row * 256 + ((r16 ^ (row & 15)) * 16)) = xb[i];
+      *reinterpret_cast<u32x4_t*>(xs + row * 256 + ((r16 ^ (row & 15)) * 16)) = xb[slot][i];
     }
+  };
+  // the features behind the last whole block, one by one, and zeros behind them
+  auto put_last_x = [&]() {
+#pragma clang loop unroll(disable)
+    for (int i = 0; i < XR * 8; ++i) {
+      const int row = i >> 1, f = (i & 1) * 64 + lane, k = whole * kI4Block + f;
+      *reinterpret_cast<uint16_t*>(xs + row * 256 + (((f >> 3) ^ (row & 15)) * 16) + (f & 7) * 2) =
+          k < p.K ? *reinterpret_cast<const uint16_t*>(x0 + ((int64_t)min(row, last_row) * p.K + k) * 2) : (uint16_t)0;
+    }
+  };
+  const I4Constants<E> constants;
+  auto multiply = [&](int slot) {
     __builtin_amdgcn_wave_barrier();
     asm volatile("" ::: "memory");
-    load_x(next_x);
     u32x4_t x[4][MT];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
@@ -170,115 +268,211 @@ __global__ void __launch_bounds__(NW * 64) gemm_i4_kernel(I4Product p) {
       }
     __builtin_amdgcn_wave_barrier();
     asm volatile("" ::: "memory");
-    float sums[G][MT];
-    if constexpr (El::kSums) {
-      const u32x4_t ones{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    f32x4_t c0[G][MT];
+    sum_block<E, G, ZEROS>(c0, x);
 #pragma unroll
-      for (int g = 0; g < G; ++g)
+    for (int j = 0; j < NT; ++j) multiply_tile<E, G, ZEROS>(tot[j], x, c0, cb[slot][j], sb[slot][j], zb[slot][j], constants);
+    // (pure arithmetic would be put off past the next blocks, with all that it needs kept in registers)
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          f32x4_t a{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int s = 0; s < kSteps; ++s) a = El::mfma(ones, x[g * kSteps + s][i], a);
-          sums[g][i] = a.x;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        uint32_t zpair = El::zero_pair(8);
-        if constexpr (ZEROS && !El::kSums) zpair = El::zero_pair(zb[slot][j].w[0] >> (8 * g) & 0xFFu);
-        f32x4_t acc[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = g * kSteps; s < (g + 1) * kSteps; ++s) {
-          const u32x4_t w = dequantise<E>(cb[slot][j][s], zpair);
-#pragma unroll
-          for (int i = 0; i < MT; ++i) acc[i] = El::mfma(w, x[s][i], acc[i]);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int at = c * G + g;
-          const float scale = half_to_float<E>(sb[slot][j].w[at >> 1], at & 1);
-          float off = -(El::kOffset + 8.f);
-          if constexpr (ZEROS && El::kSums) off = -El::kOffset - (float)(zb[slot][j].w[at >> 2] >> (8 * (at & 3)) & 0xFFu);
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            const float v = El::kSums ? fmaf(off, sums[g][i], acc[i][c]) : acc[i][c];
-            tot[i][j][c] = fmaf(scale, v, tot[i][j][c]);
-          }
-        }
-      }
-    }
+      for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(tot[j][i]));
   };
 
-  if (lo < hi) {
-    load_x(lo);
+  if (hi > whole && lo < hi) {
+    stream.load(cb[0], sb[0], zb[0], whole);
+    put_last_x();
+    multiply(0);
+  }
+  if (lo < end) {
 #pragma unroll
-    for (int d = 0; d < D; ++d) load_w(d, lo + d);
-    int b = lo;
-    for (; b + D <= hi; b += D)
+    for (int d = 0; d < D; ++d) {
+      if (d < DX) load_x(d, lo + d);
+      stream.load(cb[d], sb[d], zb[d], min(lo + d, end - 1));
+    }
+    // (one way through the loop: the compiler's waits count requests, and take the least of all ways that lead to a place)
+    for (int b = lo;; b += D)
 #pragma unroll
       for (int d = 0; d < D; ++d) {
-        block_of_features(d, b + d + 1);
-        load_w(d, b + d + D);
+        put_x(d % DX);
+        load_x(d % DX, b + d + DX);
+        multiply(d);
+        stream.load(cb[d], sb[d], zb[d], min(b + d + D, end - 1));
+        if (b + d + 1 >= end) goto done;
       }
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-      if (b + d < hi) block_of_features(d, b + d + 1);
   }
+done:
 
-  __syncthreads();
-  f32x4_t* const red = reinterpret_cast<f32x4_t*>(lds_raw);  // [wave][tile][lane]
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) red[(wave * kTiles + t) * 64 + lane] = tot[t / NT][t % NT];
-  __syncthreads();
-  for (int t = wave; t < MT * kGateTiles; t += NW) {
-    const int i = t / kGateTiles, j = t % kGateTiles;
-    auto sum = [&](int tile) {
-      f32x4_t v = red[tile * 64 + lane];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) v += red[(w * kTiles + tile) * 64 + lane];
-      return v;
-    };
-    f32x4_t v = sum(i * NT + j);
-    if constexpr (GATED) {
-      const f32x4_t up = sum(i * NT + kGateTiles + j);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = silu_tile(v[c]) * up[c];
-    }
-    const int row = row0 + i * 16 + r16, col = (tile0 + j) * 16 + 4 * q4;
-    if (row >= p.M || col >= p.N) continue;
-    const int64_t at = (int64_t)row * p.N + col;
-    if (!GATED && p.out_dtype == MDZ_FP32) store_four(reinterpret_cast<float*>(p.Y) + at, p.N - col, v);
-    else if (!GATED && p.out_dtype != (__is_same(E, bf16_t) ? MDZ_BF16 : MDZ_FP16))
-      store_four(reinterpret_cast<std::conditional_t<__is_same(E, bf16_t), f16_t, bf16_t>*>(p.Y) + at, p.N - col, v);
-    else store_four(reinterpret_cast<E*>(p.Y) + at, p.N - col, v);
-  }
+  finish_i4<E, GATED, MT, NT, 1, NW>(p, tot, reinterpret_cast<f32x4_t*>(lds_raw), row0, tile0, 0, wave, lane);
 }
 
-template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D>
-static int launch_i4_kernel(I4Product p, hipStream_t st) {
+// More rows.  A workgroup makes 16 WM MT rows x WN NT tiles of columns with WM x WN waves, WK times over: each of the WK parts has its own blocks of
+// features, and their sums meet in LDS at the end.  X, codes, scales and zero points go straight to an LDS ring (`global_load_lds`, 16 bytes
+// per lane, no registers) in turns of WK blocks; one counted wait and one barrier per turn make a turn everyone's, and behind it the place of the turn
+// that all have read is requested anew.
+template <int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int NS>
+struct I4Ring {
+  static constexpr int kWaves = WM * WN * WK, kRows = WM * MT * 16, kMats = GATED ? 2 : 1, kTiles = WN * NT / kMats;  // tiles of each matrix
+  // 1 KiB pieces of a block: X (four rows), codes (a tile), scales, zero points
+  static constexpr int kX = kRows / 4, kScales = (kTiles * 32 * G + 1023) / 1024, kZeros = ZEROS ? (kTiles * 16 * G + 1023) / 1024 : 0;
+  static constexpr int kAtScales = kX + kMats * kTiles, kAtZeros = kAtScales + kMats * kScales, kPieces = kAtZeros + kMats * kZeros;
+  static constexpr int kLoads = (WK * kPieces + kWaves - 1) / kWaves;  // per turn and wave
+  static constexpr int kTurn = WK * kPieces * 1024, kSum = WK > 1 ? kWaves * MT * NT * 1024 : 0;
+  static constexpr int kLds = NS * kTurn > kSum ? NS * kTurn : kSum;
+  static_assert(NS >= 3, "a turn is requested two turns before it is read, at least");
+};
+// a pointer that is the same in every lane, in scalar registers
+__device__ inline const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  // (the builtin gives a signed int)
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)), lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
+  return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
+}
+// all but the youngest `n` turns of L loads each have landed, for n <= NS
+template <int L, int NS>
+__device__ inline void wait_turns(int n) {
+  if (n >= NS) wait_loads<NS * L>();
+  else static_for<NS>([&](auto i) {
+    if (n == decltype(i)::value) wait_loads<decltype(i)::value * L>();
+  });
+}
+
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int NS, int WPE>
+__global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4Product p) {
+  typedef I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, NS> R;
+  constexpr int NW = R::kWaves, L = R::kLoads;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds_raw[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q4 = lane >> 4, r16 = lane & 15, wk = wave / (WM * WN), wm = wave % WM, wn = wave / WM % WN;
+  // Workgroups go round-robin to the 8 XCDs: each takes an eighth of the blocks, a column block's row blocks one after the other, which then
+  // share its weights through the XCD's L2.
+  const int xcd = blockIdx.x & 7, blocks = p.nb_m * p.nb_n;
+  const int block = (int)((int64_t)blocks * xcd >> 3) + (int)(blockIdx.x >> 3);
+  if (block >= (int)((int64_t)blocks * (xcd + 1) >> 3)) return;
+  const int row0 = block % p.nb_m * R::kRows, tile0 = block / p.nb_m * R::kTiles;
+  const int last_row = p.M - 1 - row0, last_tile = p.n_tiles - 1 - tile0, turns = (p.n_blocks + WK - 1) / WK;
+  const uint32_t lds0 = MDZ_LDS_ADDR(lds_raw);
+
+  // A wave's loads of a turn: where the piece's memory begins, a lane's place in it, how far the next block is.  (Loads beyond the last piece repeat it;
+  // rows beyond M repeat the last and tiles beyond the matrix its last: neither is stored.)  A lane of a piece of X has the 16-byte
+  // chunk of its row that stands in its place: chunk c of row r is at c ^ (r % 16), so that 16 rows' chunks are read without bank conflicts.
+  const uint8_t* base[L];
+  uint32_t off[L], chunk[L];
+  int step[L], dst[L], part[L];
+  static_for<L>([&](auto i) {
+    constexpr int q = decltype(i)::value;
+    const int u = min(q * NW + wave, WK * R::kPieces - 1), v = u % R::kPieces;
+    dst[q] = u * 1024, part[q] = u / R::kPieces;
+    if (v < R::kX) {
+      const int row = v * 4 + q4;
+      base[q] = reinterpret_cast<const uint8_t*>(p.X) + (int64_t)row0 * p.ldx, step[q] = 2 * kI4Block;
+      off[q] = (uint32_t)min(row, last_row) * (uint32_t)p.ldx, chunk[q] = (r16 ^ (row & 15)) * 16;
+    } else {
+      const int kind = v < R::kAtScales ? 0 : v < R::kAtZeros ? 1 : 2, size = kind == 0 ? 1024 : kind == 1 ? 32 * G : 16 * G;
+      const int c = v - (kind == 0 ? R::kX : kind == 1 ? R::kAtScales : R::kAtZeros), per = kind == 0 ? R::kTiles : kind == 1 ? R::kScales : max(R::kZeros, 1);
+      const I4Matrix w = GATED && c >= per ? p.w[1] : p.w[0];
+      const int at = c % per * 1024 + lane * 16, tile = min(min(at / size, R::kTiles - 1), last_tile);
+      base[q] = (kind == 0 ? w.codes : kind == 1 ? w.scales : w.zeros) + (int64_t)tile0 * p.n_blocks * size, step[q] = size;
+      off[q] = (uint32_t)tile * (uint32_t)p.n_blocks * (uint32_t)size + at % size, chunk[q] = 0;
+    }
+    base[q] = uniform(base[q]), step[q] = __builtin_amdgcn_readfirstlane(step[q]);
+    dst[q] = __builtin_amdgcn_readfirstlane(dst[q]), part[q] = __builtin_amdgcn_readfirstlane(part[q]);
+  });
+  auto request = [&](int t) {
+    const uint32_t slot = lds0 + t % NS * R::kTurn;
+    static_for<L>([&](auto i) {
+      constexpr int q = decltype(i)::value;
+      const int b = min(t * WK + part[q], p.n_blocks - 1);
+      // (the last chunk again for those beyond K, whose codes are their zero points)
+      const uint32_t o = off[q] + min(chunk[q], (uint32_t)(p.K - 8 - b * kI4Block) * 2);
+      load_to_lds<0>(base[q] + (uint32_t)(b * step[q]), o, slot + dst[q]);
+    });
+  };
+
+  f32x4_t tot[NT][MT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) tot[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const I4Constants<E> constants;
+
+  static_for<NS - 1>([&](auto i) {
+    if (decltype(i)::value < turns) request(decltype(i)::value);
+  });
+  for (int t = 0; t < turns; ++t) {
+    wait_lds();
+    wait_turns<L, NS - 2>(turns - 1 - t);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (t + NS - 1 < turns) request(t + NS - 1);
+    if (WK > 1 && t * WK + wk >= p.n_blocks) continue;
+    const uint8_t* const xs = lds_raw + t % NS * R::kTurn + wk * (R::kPieces * 1024);
+    u32x4_t x[4][MT];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        x[s][i] = *reinterpret_cast<const u32x4_t*>(xs + ((wm * MT + i) * 16 + r16) * 256 + (((s * 4 + q4) ^ r16) * 16));
+    f32x4_t c0[G][MT];
+    sum_block<E, G, ZEROS>(c0, x);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int mat = GATED && j >= NT / 2, tile = wn * (NT / R::kMats) + (GATED ? j % (NT / 2) : j);
+      const uint8_t* const cs = xs + (R::kX + mat * R::kTiles + tile) * 1024 + lane * 16;
+      const uint8_t* const ss = xs + (R::kAtScales + mat * R::kScales) * 1024 + tile * (32 * G) + q4 * (8 * G);
+      I4Zeros<G> z{};
+      if constexpr (ZEROS) z = *reinterpret_cast<const I4Zeros<G>*>(xs + (R::kAtZeros + mat * R::kZeros) * 1024 + tile * (16 * G) + q4 * (4 * G));
+      multiply_tile<E, G, ZEROS>(tot[j], x, c0, *reinterpret_cast<const u32x4_t*>(cs), *reinterpret_cast<const I4Scales<G>*>(ss), z, constants);
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(tot[j][i]));
+  }
+  finish_i4<E, GATED, MT, NT, WM * WN, WK>(p, tot, reinterpret_cast<f32x4_t*>(lds_raw), row0 + wm * MT * 16, tile0 + wn * (NT / R::kMats), wn * WM + wm, wk, lane);
+}
+
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D, int DX, int WPE>
+static int launch_i4_few(I4Product p, hipStream_t st) {
   constexpr int kGateTiles = GATED ? NT / 2 : NT;
   constexpr int kLds = NW * 1024 * (XR > MT * NT ? XR : MT * NT);
-  p.nb_m = (p.M + MT * 16 - 1) / (MT * 16), p.nb_n = (p.n_tiles + kGateTiles - 1) / kGateTiles;
-  const int64_t workgroups = ((int64_t)p.nb_m * p.nb_n + 7) / 8 * 8;
-  MDZ_REQUIRE(workgroups * NW * 64 <= (int64_t)UINT32_MAX, MDZ_EUNSUPPORTED, "linear_i4: %d x %d outputs are more than one launch takes", p.M, p.N);
-  auto kernel = gemm_i4_kernel<E, G, ZEROS, GATED, MT, NT, XR, NW, D>;
+  const int64_t columns = (p.n_tiles + kGateTiles - 1) / kGateTiles;
+  MDZ_REQUIRE(columns * NW * 64 <= (int64_t)UINT32_MAX, MDZ_EUNSUPPORTED, "linear_i4: %d columns are more than one launch takes", p.N);
+  auto kernel = gemm_i4_kernel<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>;
   MDZ_SET_LDS_ONCE(kernel, kLds);
-  launch_timed(PROF_GEMM_I4, kernel, dim3((unsigned)workgroups), NW * 64, kLds, st, p);
+  launch_timed(PROF_GEMM_I4, kernel, dim3((unsigned)columns, (p.M + MT * 16 - 1) / (MT * 16)), NW * 64, kLds, st, p);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
 }
 
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int NS, int WPE>
+static int launch_i4_rows(I4Product p, hipStream_t st) {
+  typedef I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, NS> R;
+  static_assert(R::kLds <= 160 * 1024, "LDS of a CU");
+  p.nb_m = (p.M + R::kRows - 1) / R::kRows, p.nb_n = (p.n_tiles + R::kTiles - 1) / R::kTiles;
+  const int64_t workgroups = ((int64_t)p.nb_m * p.nb_n + 7) / 8 * 8;
+  MDZ_REQUIRE(workgroups * R::kWaves * 64 <= (int64_t)UINT32_MAX, MDZ_EUNSUPPORTED, "linear_i4: %d x %d outputs are more than one launch takes", p.M, p.N);
+  auto kernel = gemm_i4_rows_kernel<E, G, ZEROS, GATED, MT, NT, WM, WN, WK, NS, WPE>;
+  MDZ_SET_LDS_ONCE(kernel, R::kLds);
+  launch_timed(PROF_GEMM_I4, kernel, dim3((unsigned)workgroups), R::kWaves * 64, R::kLds, st, p);
+  MDZ_LAUNCH_CHECK();
+  return MDZ_OK;
+}
+
+// few rows: rows / 16, tiles, pieces of X, waves; blocks of weights and of X requested ahead, waves per SIMD that the registers allow
+// more rows: rows / 16 and tiles of a wave, waves of rows, of columns and of features, turns of the ring, waves per SIMD
+#ifndef MDZ_I4_CASES
+#define MDZ_I4_CASES                 \
+  MDZ_I4_FEW(1, 2, 4, 4, 4, 4, 2)    \
+  MDZ_I4_ROWS(4, 2, 1, 4, 1, 3, 2)
+#endif
 template <typename E, int G, bool ZEROS, bool GATED>
 static int launch_i4_tiles(const I4Product& p, const I4Plan& plan, hipStream_t st) {
-#define MDZ_I4_CASE(MT, NT, XR, NW, D) \
-  if (plan.mt == MT && plan.nt == NT) return launch_i4_kernel<E, G, ZEROS, GATED, MT, NT, XR, NW, D>(p, st);
-  MDZ_I4_CASE(1, 2, 4, 4, 4)
-  MDZ_I4_CASE(4, 2, 16, 4, 2)
+#define MDZ_I4_FEW(MT, NT, XR, NW, D, DX, WPE) \
+  if (plan.wn == 0 && plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.wk == NW) return launch_i4_few<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>(p, st);
+#define MDZ_I4_ROWS(MT, NT, WM, WN, WK, NS, WPE) \
+  if (plan.mt == MT && plan.nt == NT && plan.wm == WM && plan.wn == WN && plan.wk == WK) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, WM, WN, WK, NS, WPE>(p, st);
+  MDZ_I4_CASES
   MDZ_FAIL(MDZ_EINVAL, "linear_i4: no kernel of %d x %d tiles", plan.mt, plan.nt);
 }
 

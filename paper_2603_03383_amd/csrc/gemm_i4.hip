@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(256) pack_i4_kernel(I4Source s, int64_t n_rows
   uint32_t word = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) word |= (uint32_t)q[e] << (4 * i4_field(e));
-  codes[w] = word << 3 | word >> 29;
+  codes[w] = word << kI4Rotation<E> | word >> (32 - kI4Rotation<E>);
   if (in_block % group == 0) {
     const int64_t to = (at * 16 + r) * (kI4Block / group) + in_block / group;
     scales[to] = from_float<E>(scale);
@@ -97,7 +97,22 @@ static int pack_i4(int dtype, const I4Source& s, int64_t n_rows, int64_t k, int 
 }
 
 // ---- products ----------------------------------------------------------------------------------------
-static I4Plan plan_i4(int M, int N, int K, bool gated) { return I4Plan{M <= 16 ? 1 : 4, 2}; }
+static I4Plan plan_i4(int M, int N, int K, bool gated) { return M <= 16 ? I4Plan{1, 2, 0, 0, 4, 4} : I4Plan{4, 2, 1, 4, 1, 0}; }
+
+// Rows that do not start on 16 bytes, again 16 bytes apart and padded with zeros to whole blocks: a thread makes eight features.
+__global__ void __launch_bounds__(256) align_rows_i4_kernel(const uint16_t* __restrict__ x, int K, u32x4_t* __restrict__ out, int64_t chunks, int per_row) {
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (q >= chunks) return;
+  const int64_t row = q / per_row;
+  const int k = (int)(q - row * per_row) * 8;
+  u32x4_t v{0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (k + e < K) v[e >> 1] |= (uint32_t)x[row * K + k + e] << (16 * (e & 1));
+  out[q] = v;
+}
+// scratch for them
+static int64_t aligned_bytes_i4(int M, int K) { return M <= 16 ? 0 : (int64_t)M * i4_blocks(K) * kI4Block * 2; }
 
 static int check_product_i4(const char* what, int M, int N, int K) {
   MDZ_REQUIRE(M >= 0 && N > 0 && K > 0, MDZ_EINVAL, "%s: [%d,%d] x [%d,%d]", what, M, K, N, K);
@@ -122,9 +137,21 @@ static int product_i4(const char* what, int dtype, const void* x, const void* pa
   I4Product p{};
   p.X = x, p.w[0] = i4_matrix(packed, N, K, group), p.w[1] = i4_matrix(second ? second : packed, N, K, group), p.Y = y;
   p.M = M, p.N = N, p.K = K, p.out_dtype = out_dtype, p.n_tiles = (int)i4_tiles(N), p.n_blocks = (int)i4_blocks(K);
+  const int64_t need = aligned_bytes_i4(M, K);
+  MDZ_REQUIRE(ws_bytes >= need && (ws || need == 0), MDZ_EWORKSPACE, "%s: workspace %lld < %lld bytes", what, (long long)ws_bytes, (long long)need);
+  MDZ_REQUIRE(need == 0 || (reinterpret_cast<uintptr_t>(ws) & 15) == 0, MDZ_EINVAL, "%s: the workspace must start on 16 bytes", what);
   const I4Plan plan = plan_i4(M, N, K, second != nullptr);
   hipStream_t st = (hipStream_t)stream;
   const bool z = zeros != 0, gated = second != nullptr;
+  p.ldx = (int64_t)K * 2;
+  if (plan.wm > 0 && (K % 8 != 0 || reinterpret_cast<uintptr_t>(x) % 16 != 0)) {  // loads to LDS take 16 bytes from addresses of 16
+    const int64_t chunks = need / 16;
+    MDZ_REQUIRE(chunks <= (int64_t)UINT32_MAX - 255, MDZ_EUNSUPPORTED, "%s: %d unaligned rows are more than one launch takes", what, M);
+    launch_timed(PROF_GEMM_I4, align_rows_i4_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, (const uint16_t*)x, K, (u32x4_t*)ws, chunks,
+                 p.n_blocks * (kI4Block / 8));
+    MDZ_LAUNCH_CHECK();
+    p.X = ws, p.K = p.n_blocks * kI4Block, p.ldx = (int64_t)p.K * 2;
+  }
   MDZ_WITH_ELEM16(dtype, return (group == 128 ? launch_i4<E, 1>(p, z, gated, plan, st) : group == 64 ? launch_i4<E, 2>(p, z, gated, plan, st)
                                                                                                   : launch_i4<E, 4>(p, z, gated, plan, st)));
 }
@@ -151,9 +178,15 @@ int medusa_pack_codes_i4(int dtype, const uint8_t* codes, const void* scales, co
   return pack_i4(dtype, I4Source{nullptr, codes, scales, zeros_opt}, n_rows, k, group, zeros_opt != nullptr, dst, dst_rows, tile_offset, stream);
 }
 
-int64_t medusa_linear_i4_workspace_bytes(int M, int N, int K) { return check_product_i4("linear_i4", M, N, K); }
+int64_t medusa_linear_i4_workspace_bytes(int M, int N, int K) {
+  const int rc = check_product_i4("linear_i4", M, N, K);
+  return rc ? rc : aligned_bytes_i4(M, K);
+}
 
-int64_t medusa_swiglu_i4_workspace_bytes(int M, int ffn, int K) { return check_product_i4("swiglu_i4", M, ffn, K); }
+int64_t medusa_swiglu_i4_workspace_bytes(int M, int ffn, int K) {
+  const int rc = check_product_i4("swiglu_i4", M, ffn, K);
+  return rc ? rc : aligned_bytes_i4(M, K);
+}
 
 int medusa_linear_i4(int dtype, const void* x, const void* packed, int M, int N, int K, int group, int zeros, int out_dtype, void* y, void* ws,
                      int64_t ws_bytes, void* stream) {

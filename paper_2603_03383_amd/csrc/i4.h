@@ -9,8 +9,8 @@ namespace mdz {
 //           32 s + 8 (l / 16) .. +7 of the block, so a wave loads a block with one instruction and a tile is one contiguous stream.
 //   scales: [tile][block][16 rows][groups of the block], 16-bit; the products leave a lane with rows 4 (l / 16) .. +3, whose scales lie together.
 //   zeros:  (only in matrices that have zero points) the same order, a byte each.
-// The eight codes of a word stand in fields of four bits, feature e of them in field e / 2 + 4 (e % 2), and the word is rotated left by three:
-// two features are then one mask away from a pair of 16-bit floating numbers with the code in the mantissa's bits 3 .. 6 (see dequantise).
+// The eight codes of a word stand in fields of four bits, feature e of them in field e / 2 + 4 (e % 2), and the word is rotated left by three (bf16) or
+// six (binary16): two features are then one mask away from a pair of 16-bit floating numbers with the code at the top of the mantissa (see dequantise).
 // Features are padded to 128 with codes equal to their zero points and rows to 16 with scales of zero.
 constexpr int kI4TileRows = MDZ_I4_TILE_ROWS;
 constexpr int kI4Block = 128;
@@ -27,6 +27,8 @@ __host__ __device__ inline int64_t i4_packed_bytes(int64_t n, int64_t k, int gro
 inline bool i4_group_ok(int group) { return group == 32 || group == 64 || group == 128; }
 // place of a word's feature e among the fields of four bits before the rotation
 __host__ __device__ inline int i4_field(int e) { return (e >> 1) + 4 * (e & 1); }
+template <typename E>
+constexpr int kI4Rotation = __is_same(E, f16_t) ? 6 : 3;
 
 // One matrix of a product.
 struct I4Matrix {
@@ -45,13 +47,15 @@ struct I4Product {
   I4Matrix w[2];
   void* Y;
   int M, N, K, out_dtype;
+  int64_t ldx;  // bytes from row to row of X
   int n_tiles, n_blocks;
   int nb_m, nb_n;  // workgroups of rows and of columns
 };
 
-// How a product is cut: rows and tiles of a workgroup (of a gated product: pairs of tiles).
+// How a product is cut: rows / 16 and tiles (a gated product's are half gate, half up) of a wave, waves of rows (0: the kernel of few rows), of columns and of
+// features, and for few rows the pieces of four of them that are loaded.
 struct I4Plan {
-  int mt, nt;
+  int mt, nt, wm, wn, wk, xr;
 };
 template <typename E, int G>
 int launch_i4(const I4Product& p, bool zeros, bool gated, const I4Plan& plan, hipStream_t st);
