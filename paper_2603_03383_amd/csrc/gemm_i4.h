@@ -319,7 +319,7 @@ struct I4Ring {
   static constexpr int kLoads = (WK * kPieces + kWaves - 1) / kWaves;  // per turn and wave
   static constexpr int kTurn = WK * kPieces * 1024, kSum = WK > 1 ? kWaves * MT * NT * 1024 : 0;
   static constexpr int kLds = NS * kTurn > kSum ? NS * kTurn : kSum;
-  static_assert(NS >= 3, "a turn is requested two turns before it is read, at least");
+  static_assert(NS >= 2, "a turn is requested before it is read");
 };
 // a pointer that is the same in every lane, in scalar registers
 __device__ inline const uint8_t* uniform(const uint8_t* p) {
@@ -445,8 +445,10 @@ static int launch_i4_few(I4Product p, hipStream_t st) {
   return MDZ_OK;
 }
 
-template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int NS, int WPE>
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int WPE>
 static int launch_i4_rows(I4Product p, hipStream_t st) {
+  // (three turns fit but for the widest tiles in groups of 32 with zero points)
+  constexpr int NS = I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, 3>::kLds <= 160 * 1024 ? 3 : 2;
   typedef I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, NS> R;
   static_assert(R::kLds <= 160 * 1024, "LDS of a CU");
   p.nb_m = (p.M + R::kRows - 1) / R::kRows, p.nb_n = (p.n_tiles + R::kTiles - 1) / R::kTiles;
@@ -460,18 +462,36 @@ static int launch_i4_rows(I4Product p, hipStream_t st) {
 }
 
 // few rows: rows / 16, tiles, pieces of X, waves; blocks of weights and of X requested ahead, waves per SIMD that the registers allow
-// more rows: rows / 16 and tiles of a wave, waves of rows, of columns and of features, turns of the ring, waves per SIMD
-#ifndef MDZ_I4_CASES
-#define MDZ_I4_CASES                 \
-  MDZ_I4_FEW(1, 2, 4, 4, 4, 4, 2)    \
-  MDZ_I4_ROWS(4, 2, 1, 4, 1, 3, 2)
-#endif
+// more rows: rows / 16 and tiles of a wave, waves of rows, of columns and of features, waves per SIMD
+#define MDZ_I4_CASES                    \
+  MDZ_I4_FEW(1, 1, 1, 8, 8, 8, 2)       \
+  MDZ_I4_FEW(1, 2, 1, 8, 4, 4, 2)       \
+  MDZ_I4_FEW(1, 2, 1, 4, 6, 6, 2)       \
+  MDZ_I4_FEW(1, 4, 1, 4, 4, 4, 2)       \
+  MDZ_I4_FEW(1, 1, 2, 8, 5, 5, 2)       \
+  MDZ_I4_FEW(1, 2, 2, 8, 4, 4, 2)       \
+  MDZ_I4_FEW(1, 2, 2, 4, 5, 5, 2)       \
+  MDZ_I4_FEW(1, 4, 2, 4, 4, 4, 2)       \
+  MDZ_I4_FEW(1, 1, 4, 8, 4, 4, 2)       \
+  MDZ_I4_FEW(1, 2, 4, 8, 3, 3, 2)       \
+  MDZ_I4_FEW(1, 2, 4, 4, 4, 4, 2)       \
+  MDZ_I4_FEW(1, 4, 4, 4, 3, 3, 2)       \
+  MDZ_I4_FEW(2, 1, 8, 8, 3, 1, 2)       \
+  MDZ_I4_FEW(2, 2, 8, 8, 3, 1, 2)       \
+  MDZ_I4_FEW(2, 6, 8, 4, 3, 1, 1)       \
+  MDZ_I4_FEW(4, 1, 16, 8, 4, 1, 2)      \
+  MDZ_I4_FEW(4, 2, 16, 8, 2, 1, 2)      \
+  MDZ_I4_FEW(4, 6, 16, 4, 2, 1, 1)      \
+  MDZ_I4_ROWS(4, 2, 1, 4, 1, 2)         \
+  MDZ_I4_ROWS(4, 4, 1, 8, 1, 2)
 template <typename E, int G, bool ZEROS, bool GATED>
 static int launch_i4_tiles(const I4Product& p, const I4Plan& plan, hipStream_t st) {
-#define MDZ_I4_FEW(MT, NT, XR, NW, D, DX, WPE) \
-  if (plan.wn == 0 && plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.wk == NW) return launch_i4_few<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>(p, st);
-#define MDZ_I4_ROWS(MT, NT, WM, WN, WK, NS, WPE) \
-  if (plan.mt == MT && plan.nt == NT && plan.wm == WM && plan.wn == WN && plan.wk == WK) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, WM, WN, WK, NS, WPE>(p, st);
+#define MDZ_I4_FEW(MT, NT, XR, NW, D, DX, WPE)                                                        \
+  if constexpr (!GATED || NT % 2 == 0)                                                                \
+    if (plan.wm == 0 && plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.wk == NW)              \
+      return launch_i4_few<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>(p, st);
+#define MDZ_I4_ROWS(MT, NT, WM, WN, WK, WPE) \
+  if (plan.mt == MT && plan.nt == NT && plan.wm == WM && plan.wn == WN && plan.wk == WK) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, WM, WN, WK, WPE>(p, st);
   MDZ_I4_CASES
   MDZ_FAIL(MDZ_EINVAL, "linear_i4: no kernel of %d x %d tiles", plan.mt, plan.nt);
 }

@@ -97,7 +97,39 @@ static int pack_i4(int dtype, const I4Source& s, int64_t n_rows, int64_t k, int 
 }
 
 // ---- products ----------------------------------------------------------------------------------------
-static I4Plan plan_i4(int M, int N, int K, bool gated) { return M <= 16 ? I4Plan{1, 2, 0, 0, 4, 4} : I4Plan{4, 2, 1, 4, 1, 0}; }
+// Up to 16 rows the weights are the stream and each workgroup of the kernel of few rows takes one column tile (pair) until every CU has one, with eight waves on
+// its features, then two and four with four waves.  (us at 1 row, one / two / four tiles: 4096 x 4096 5.4 / 6.5 / 8.4; 12288 x 4096 9.1 / 9.7 / 8.9;
+// 128000 x 4096 72.6 / 59.8 / 56.7; 16 rows 12288 x 4096 17.2 / 11.9 / 9.9; gated 688 pairs, one / two: 14.3 / 15.2 at 1 row, 18.3 / 16.8 at 16.)
+// Beyond, the cut of the least modelled time: rounds of workgroups over the chip x turns of a workgroup x a turn's us, measured on full chips.
+static I4Plan plan_i4(int M, int N, int K, bool gated) {
+  const int64_t tiles = i4_tiles(N), blocks = i4_blocks(K), cus = num_cus();
+  if (M <= 16) {
+    const int xr = M <= 4 ? 1 : M <= 8 ? 2 : 4;
+    if (gated) return tiles <= cus ? I4Plan{1, 2, 0, 0, 8, xr} : tiles <= 4 * cus && xr < 4 ? I4Plan{1, 2, 0, 0, 4, xr} : I4Plan{1, 4, 0, 0, 4, xr};
+    return tiles <= cus ? I4Plan{1, 1, 0, 0, 8, xr} : tiles <= 2 * cus ? I4Plan{1, 2, 0, 0, 4, xr} : I4Plan{1, 4, 0, 0, 4, xr};
+  }
+  struct Cut {
+    I4Plan plan;
+    int least_rows, most_rows, rows, tiles, gate_tiles, features, resident;  // features: blocks of a turn; resident: workgroups of a CU
+    float us;
+  };
+  static constexpr Cut kCuts[] = {
+      {{2, 1, 0, 0, 8, 8}, 17, 32, 32, 1, 0, 8, 1, 1.5f},   {{2, 2, 0, 0, 8, 8}, 17, 32, 32, 2, 1, 8, 1, 2.2f},
+      {{2, 6, 0, 0, 4, 8}, 17, 32, 32, 6, 3, 4, 1, 1.9f},   {{4, 1, 0, 0, 8, 16}, 33, 1 << 30, 64, 1, 0, 8, 1, 2.1f},
+      {{4, 2, 0, 0, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, 1, 2.9f}, {{4, 6, 0, 0, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, 1, 2.7f},
+      {{4, 2, 1, 4, 1, 0}, 17, 1 << 30, 64, 8, 4, 1, 2, 1.5f},  {{4, 4, 1, 8, 1, 0}, 17, 1 << 30, 64, 32, 16, 1, 1, 2.4f},
+  };
+  I4Plan best{};
+  float least = INFINITY;
+  for (const Cut& c : kCuts) {
+    const int wide = gated ? c.gate_tiles : c.tiles;
+    if (M < c.least_rows || M > c.most_rows || wide == 0) continue;
+    const int64_t wgs = ((M + c.rows - 1) / c.rows) * ((tiles + wide - 1) / wide), at_once = cus * c.resident;
+    const float us = (float)((wgs + at_once - 1) / at_once * ((blocks + c.features - 1) / c.features)) * c.us;
+    if (us < least) best = c.plan, least = us;
+  }
+  return best;
+}
 
 // Rows that do not start on 16 bytes, again 16 bytes apart and padded with zeros to whole blocks: a thread makes eight features.
 __global__ void __launch_bounds__(256) align_rows_i4_kernel(const uint16_t* __restrict__ x, int K, u32x4_t* __restrict__ out, int64_t chunks, int per_row) {
