@@ -282,6 +282,28 @@ int64_t medusa_swiglu_i4_workspace_bytes(int M, int ffn, int K);
 int medusa_swiglu_i4(int dtype, const void* x, const void* gate_packed, const void* up_packed, int M, int ffn, int K, int group,
                      int zeros, void* y, void* ws, int64_t ws_bytes, void* stream);
 
+/* ---- sampling ------------------------------------------------------------------------------- */
+
+/* One token for each of `rows` rows of `vocab` logits (type dtype, rows ld >= vocab elements apart) from given random
+ * numbers u [rows] in [0, 1).  A row's tokens in the order of their logits, descending, ties to the lower index; a token's mass
+ * is exp((logit - largest) / temperature).  top_k: the first k tokens are kept (k <= 0: all).  top_p: of those, the tokens
+ * before which less than top_p of their mass lies, the first always (top_p >= 1: all).  min_p: of those, the tokens whose mass is
+ * at least min_p times the largest's (min_p <= 0: all; at most 1 counts).  token [rows] receives the first kept token up to and
+ * with which more than u of the kept mass lies, prob_opt (nullable) [rows] its share of the kept mass.  A temperature that is
+ * not above zero stands for the row's first token.  NaN and minus infinity cannot be drawn; beside plus infinity nothing else
+ * can; a row in which nothing can be drawn gets token -1 and prob 0.  u outside [0, 1) is taken as its nearer end.
+ * Settings lie in device memory, one for every rows_per_setting rows in a row (a tree's nodes): [ceil(rows / rows_per_setting)] each;
+ * NULL: temperature 1, no top-k, no top-p, no min-p.  Masses are 64-bit integers in steps of at most 2^-(61 - b) of the largest, b the bits of
+ * vocab (at most 2^24), and their sums are exact: a row's token depends on nothing but the row.
+ * Drawn at every node of a tree, the tokens take node_argmax's place in accept_longest_prefix: the path is then one that
+ * sampling token by token gives with these random numbers, and next_root the token drawn after it.
+ * ws: medusa_sample_workspace_bytes(rows, vocab) bytes of scratch that start on 16 bytes (0: ws may be NULL); nothing in it has
+ * to be set, and nothing is kept in it. */
+int64_t medusa_sample_workspace_bytes(int rows, int vocab);
+int medusa_sample(int dtype, const void* logits, int64_t ld, int rows, int vocab, const float* temperature_opt,
+                  const int32_t* top_k_opt, const float* top_p_opt, const float* min_p_opt, int rows_per_setting,
+                  const float* u, int32_t* token, float* prob_opt, void* ws, int64_t ws_bytes, void* stream);
+
 /* ---- KV cache ------------------------------------------------------------------------------- */
 
 /* Bytes of EACH of desc->k and desc->v (negative = mdz_status). */
@@ -355,7 +377,8 @@ int tree_verify_step(const mdz_model_desc* model, const mdz_weights* w, const in
  * tree_tokens[n] == node_argmax[parent[n]]; the root always matches.  For every row of the retrieve
  * table count the leading matching nodes; best_path = the longest (ties -> lowest row index),
  * accept_len A in [1, K+1].  acc_nodes / acc_tokens [B, K+1] = first A nodes of that row and their
- * tokens, -1 padded; last_node = acc_nodes[A-1]; next_root = node_argmax[last_node]. */
+ * tokens, -1 padded; last_node = acc_nodes[A-1]; next_root = node_argmax[last_node].  (Tokens that medusa_sample drew at the
+ * nodes may stand in node_argmax: the path of drawn tokens is then accepted.) */
 int accept_longest_prefix(int tree, const int32_t* tree_tokens, const int32_t* node_argmax, int B,
                           int32_t* accept_len, int32_t* best_path, int32_t* acc_nodes, int32_t* acc_tokens,
                           int32_t* next_root, int32_t* last_node, void* stream);

@@ -7,5 +7,5 @@ from .binding import (EXPORTED, LIB_PATH, MDZ_BF16, MDZ_FP32, MDZ_FP16, MDZ_KV_P
 from .binding import (MDZ_I8_TILE_ROWS, medusa_linear_i8, medusa_linear_i8_parts_plan, medusa_linear_i8_plan, medusa_linear_i8_workspace_bytes, medusa_pack_codes_i8, medusa_pack_weight_i8,
                       medusa_packed_i8_bytes, medusa_quantize_rows_i8, medusa_residual_rmsnorm_i8, medusa_swiglu_i8, medusa_test_i8_update_norm)
 from .binding import (MDZ_I4_TILE_ROWS, medusa_linear_i4, medusa_linear_i4_workspace_bytes, medusa_pack_codes_i4, medusa_pack_weight_i4, medusa_packed_i4_bytes,
-                      medusa_swiglu_i4, medusa_swiglu_i4_workspace_bytes)
-from .runtime import ChainedDecoder, DeviceKV, DeviceModel, StepBuffers, run_step
+                      medusa_sample, medusa_sample_workspace_bytes, medusa_swiglu_i4, medusa_swiglu_i4_workspace_bytes)
+from .runtime import ChainedDecoder, DeviceKV, DeviceModel, Sampling, StepBuffers, run_step

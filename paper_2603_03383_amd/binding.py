@@ -97,6 +97,8 @@ _SIGNATURES = {
     "medusa_linear_i4": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p] + [C.c_int] * 6 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "medusa_swiglu_i4_workspace_bytes": (C.c_int64, [C.c_int] * 3),
     "medusa_swiglu_i4": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int] * 5 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "medusa_sample_workspace_bytes": (C.c_int64, [C.c_int] * 2),
+    "medusa_sample": (C.c_int, [C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_int] + [C.c_void_p] * 4 + [C.c_int] + [C.c_void_p] * 4 + [C.c_int64, C.c_void_p]),
     "medusa_kv_bytes": (C.c_int64, [C.POINTER(KvDesc)]),
     "medusa_kv_init": (C.c_int, [C.POINTER(KvDesc), C.c_void_p]),
     "medusa_test_force_unfused_rope": (C.c_int, [C.c_int]),
@@ -479,6 +481,32 @@ def medusa_swiglu_i4(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, grou
         dtype, _operand("x", x, x.shape, x.dtype, gpu), _packed_i4("gate", gate, N, K, group, zeros, gpu), _packed_i4("up", up, N, K, group, zeros, gpu),
         M, N, K, group, int(zeros), _operand("y", y, (M, N), x.dtype, gpu), None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu),
         0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
+
+
+# ---------------------------------------------------------------------------------------------
+# sampling
+# ---------------------------------------------------------------------------------------------
+def medusa_sample_workspace_bytes(rows: int, vocab: int) -> int:
+    _int32("sample", rows, vocab)
+    return _check(lib().medusa_sample_workspace_bytes(rows, vocab))
+
+
+def medusa_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor, prob: Optional[torch.Tensor] = None, *, temperature=None, top_k=None,
+                  top_p=None, min_p=None, rows_per_setting: int = 1, ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """logits [rows, vocab] of a storage dtype (rows may lie further apart), u fp32 [rows] -> token int32 [rows], prob fp32 [rows] (optional).  The settings:
+    device tensors [ceil(rows / rows_per_setting)], top_k int32 and the others fp32, or None."""
+    (rows, vocab), dtype, gpu = _rows("logits", logits)
+    if rows_per_setting <= 0 or rows_per_setting >> 31:
+        raise MedusaError(-1, f"sample: {rows_per_setting} rows per setting")
+    ld = logits.stride(0) if rows > 1 else vocab
+    if (vocab > 1 and logits.stride(1) != 1) or ld < vocab:
+        raise MedusaError(-2, "logits: a row's logits must lie side by side, and rows must not overlap")
+    n, f32 = (-(-rows // rows_per_setting),), torch.float32
+    _check(lib().medusa_sample(
+        dtype, logits.data_ptr(), ld, rows, vocab, _operand("temperature", temperature, n, f32, gpu), _operand("top_k", top_k, n, torch.int32, gpu),
+        _operand("top_p", top_p, n, f32, gpu), _operand("min_p", min_p, n, f32, gpu), rows_per_setting, _operand("u", u, (rows,), f32, gpu),
+        _operand("token", token, (rows,), torch.int32, gpu), _operand("prob", prob, (rows,), f32, gpu),
+        None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu), 0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
 
 
 def medusa_kv_bytes(kv: KvDesc) -> int:

@@ -228,15 +228,41 @@ class StepBuffers:
         self.kv_src_slots = torch.zeros(batch, K + 1, **i32)
 
 
+class Sampling:
+    """Sampled decoding: the settings of a batch's sequences (numbers, or one per sequence; None: not used) and the random numbers of
+    a step, `u` [batch, T] in [0, 1), one for each node of each tree, which the caller fills before every step."""
+
+    def __init__(self, model: DeviceModel, batch: int, temperature=None, top_k=None, top_p=None, min_p=None):
+        def each(v, dtype):
+            if v is None:
+                return None
+            return torch.as_tensor(v, dtype=dtype).expand(batch).to(model.device).contiguous()
+        T, V = model.tree_info["T"], model.desc.vocab
+        self.settings = dict(temperature=each(temperature, torch.float32), top_k=each(top_k, torch.int32),
+                             top_p=each(top_p, torch.float32), min_p=each(min_p, torch.float32), rows_per_setting=T)
+        self.u = torch.zeros(batch, T, dtype=torch.float32, device=model.device)
+        self.prob = torch.zeros(batch, T, dtype=torch.float32, device=model.device)
+        self.ws = torch.empty(B.medusa_sample_workspace_bytes(batch * T, V), dtype=torch.uint8, device=model.device)
+
+    def draw(self, logits: torch.Tensor, tokens: torch.Tensor, stream=None) -> None:
+        """logits [batch, T, vocab] -> tokens [batch, T] (and their probabilities, in `prob`)."""
+        B.medusa_sample(logits.flatten(0, 1), self.u.flatten(), tokens.flatten(), self.prob.flatten(), ws=self.ws, stream=stream, **self.settings)
+
+
 def run_step(model: DeviceModel, kv: DeviceKV, buf: StepBuffers, hidden, src_row, root_token, seq_len,
-             with_heads: bool = True, stream=None) -> None:
-    """Enqueues heads -> verify -> accept -> compact (the four C-ABI calls, nothing else)."""
+             with_heads: bool = True, stream=None, sampling: Optional[Sampling] = None) -> None:
+    """Enqueues heads -> verify -> accept -> compact (the four C-ABI calls, nothing else).  With `sampling` the tokens that the
+    model gives at the nodes are drawn from its logits (buf needs them: want_logits) and take the place of the likeliest."""
     Bn = buf.batch
     if with_heads:
         B.medusa_heads(model.desc, model.weights, hidden, src_row, root_token, Bn, hidden.shape[1], buf.cand_flat,
                        buf.tree_tokens, buf.head_logits, buf.ws, stream)
     B.tree_verify_step(model.desc, model.weights, buf.tree_tokens, kv.desc, seq_len, Bn, buf.max_prefix,
                        buf.node_argmax, buf.hidden, buf.logits, buf.ws, stream)
+    if sampling is not None:
+        if buf.logits is None:
+            raise B.MedusaError(-1, "sampling: the step's buffers hold no logits (want_logits)")
+        sampling.draw(buf.logits, buf.node_argmax, stream)
     B.accept_longest_prefix(model.tree, buf.tree_tokens, buf.node_argmax, Bn, buf.accept_len, buf.best_path,
                             buf.acc_nodes, buf.acc_tokens, buf.next_root, buf.last_node, stream)
     B.kv_compact(kv.desc, model.tree, buf.acc_nodes, buf.accept_len, seq_len, buf.kv_src_slots, Bn, buf.max_prefix,
@@ -247,12 +273,13 @@ class ChainedDecoder:
     """Speculative steps enqueued back to back with no host round trip (the paper's static-shape, device-resident
     decode loop, Section 3.2): step i's heads read step i-1's hidden state at `last_node`, its root is step i-1's
     `next_root`, and the sequence lengths live on the device.  With ``use_graph`` one step is captured in a HIP graph
-    and replayed.  Only argument marshalling and buffer bookkeeping happen here; every step of the method runs in the
+    and replayed.  With ``sampling`` the tokens are drawn, from the random numbers given to ``run``.  Only argument marshalling and buffer bookkeeping happen here; every step of the method runs in the
     library's kernels."""
 
-    def __init__(self, model: DeviceModel, kv: DeviceKV, batch: int, max_prefix: int, use_graph: bool = True):
-        self.model, self.kv, self.batch = model, kv, batch
-        self.buf = StepBuffers(model, batch, max_prefix)
+    def __init__(self, model: DeviceModel, kv: DeviceKV, batch: int, max_prefix: int, use_graph: bool = True,
+                 sampling: Optional[Sampling] = None):
+        self.model, self.kv, self.batch, self.sampling = model, kv, batch, sampling
+        self.buf = StepBuffers(model, batch, max_prefix, want_logits=sampling is not None)
         self.seq_len = torch.zeros(batch, dtype=torch.int32, device=model.device)
         self.use_graph = use_graph
         self._graph = None
@@ -269,7 +296,7 @@ class ChainedDecoder:
 
     def _step(self) -> None:
         b = self.buf
-        run_step(self.model, self.kv, b, b.hidden, b.last_node, b.next_root, self.seq_len)
+        run_step(self.model, self.kv, b, b.hidden, b.last_node, b.next_root, self.seq_len, sampling=self.sampling)
 
     def _capture(self) -> None:
         b = self.buf
@@ -289,16 +316,21 @@ class ChainedDecoder:
         for t, s in zip((b.hidden, b.last_node, b.next_root, self.seq_len), saved):
             t.copy_(s)                                     # capture does not run the kernels; restore anyway
 
-    def run(self, n_steps: int):
+    def run(self, n_steps: int, u: Optional[torch.Tensor] = None):
         """Enqueues n_steps steps; returns device tensors (tokens [n_steps, B, K+1] with -1 padding,
-        accept_len [n_steps, B]).  The caller synchronises when it wants to read them."""
+        accept_len [n_steps, B]).  The caller synchronises when it wants to read them.  With sampling, u [n_steps, B, T]: the
+        random numbers, one for each node of each step's trees."""
         b = self.buf
+        if (self.sampling is None) != (u is None) or (u is not None and u.shape != (n_steps, *self.sampling.u.shape)):
+            raise B.MedusaError(-2, "run: u [n_steps, batch, nodes] belongs to a decoder that samples, and to no other")
         K1 = b.acc_tokens.shape[1]
         tokens = torch.empty(n_steps, self.batch, K1, dtype=torch.int32, device=self.model.device)
         lens = torch.empty(n_steps, self.batch, dtype=torch.int32, device=self.model.device)
         if self.use_graph and self._graph is None:
             self._capture()
         for i in range(n_steps):
+            if u is not None:
+                self.sampling.u.copy_(u[i])
             if self._graph is not None:
                 self._graph.replay()
             else:
