@@ -6,8 +6,9 @@
 // token up to which p of that lies, min-p the mass of the logits from a border on; the kept tokens are the shortest of these beginnings, and the draw is the
 // token at which the running sum passes u times their mass.  So nothing is sorted but the bin of a histogram in which such a place lies.
 //
-// Bins: 1024 steps of (largest - logit) / temperature, 1/32 each.  A place is found in the bins' running sums; of its bin the tokens are gathered and
-// sorted, or, where they are more than kSortMost (ties, flat rows), cut again by their bits into 1024 until they are few or all equal.
+// Bins: 1024 steps of (largest - logit) / temperature, 1/32 each.  A place is found in the bins' running sums; its bin is cut again by the bits of its
+// logits into 1024, until it holds up to 64 tokens, which a wave sorts, or equal ones, which are counted.  Which bins the places of a row can
+// lie in follows from the running sums alone, so their tokens are read once, into LDS (up to kCandidates; from memory each time beyond that).
 #include "kernels.h"
 
 namespace mdz {
@@ -15,8 +16,10 @@ namespace mdz {
 constexpr int kBins = 1024;
 constexpr float kBinsPerUnit = 32.f;
 constexpr int kChunk = 4096;      // tokens of a workgroup where a row is split
-constexpr int kSortMost = 2048;   // tokens of a bin that are sorted in LDS
+constexpr int kSortMost = 64;     // tokens that a wave sorts
+constexpr int kCandidates = 4096;  // tokens of the places' bins in LDS
 constexpr int kMaskWords = kBins / 32;
+constexpr int kChunkList = 256;   // chunks of a row whose masks are looked at together
 
 struct SampleArgs {
   const void* logits;
@@ -38,28 +41,27 @@ struct SampleArgs {
 
 // a row's settings, and the largest of its logits
 struct RowSettings {
-  float inv_t, largest;
-  double rate;  // log2(e) / temperature
+  float per_unit, largest, top;  // bins per unit of logits; top: the largest, or the largest number below plus infinity
+  double rate;                   // log2(e) / temperature
   int top_k, shift;
-  double top_p, min_p;
-  __device__ inline RowSettings(const SampleArgs& a, int row, float max) {
+  double top_p, min_p, u;
+  __device__ inline RowSettings(const SampleArgs& a, int row) {
     const int s = row / a.per;
     const float t = a.temperature ? a.temperature[s] : 1.f;
     const bool greedy = !(t > 0.f);
-    largest = max, shift = a.shift;
-    inv_t = greedy ? 1.f : fminf(1.f / t, 3.402823466e38f);
+    shift = a.shift;
+    per_unit = greedy ? kBinsPerUnit : fminf(1.f / t * kBinsPerUnit, 3.402823466e38f);
     rate = greedy ? 1.4426950408889634 : 1.4426950408889634 / (double)t;
     top_k = greedy ? 1 : a.top_k ? a.top_k[s] : 0;
     top_p = a.top_p ? (double)a.top_p[s] : 1.0;
     min_p = a.min_p ? (double)a.min_p[s] : 0.0;
+    u = (double)a.u[row];
   }
+  __device__ inline void set_largest(float max) { largest = max, top = fminf(max, 3.402823466e38f); }
   // tokens that can be drawn: not NaN, not minus infinity; beside plus infinity nothing else
   __device__ inline bool valid(float l) const { return l > -INFINITY && (largest < INFINITY || l == largest); }
-  // monotone in l: a difference, a product and a conversion of fp32
-  __device__ inline int bin(float l) const {
-    const float d = l == largest ? 0.f : fminf(largest - l, 3.402823466e38f) * inv_t;
-    return (int)fminf(d * kBinsPerUnit, (float)(kBins - 1));
-  }
+  // Monotone in l (a difference, a product and a conversion of fp32); what is not valid is somewhere among the bins too.
+  __device__ inline int bin(float l) const { return (int)fmaxf(fminf((top - l) * per_unit, (float)(kBins - 1)), 0.f); }
   // 2^(shift + y), rounded to an integer; 2^f by its series, whose rest behind f^11 is below 7e-15 (the masses' steps are 2^-45 at 128000 tokens)
   __device__ inline uint64_t mass(float l) const {
     const double diff = l == largest ? 0.0 : (double)l - (double)largest;
@@ -84,6 +86,46 @@ struct RowSettings {
 // logit i of a row (minus zero as zero: they tie)
 template <typename T>
 __device__ inline float logit(const T* row, int i) { return to_float(row[i]) + 0.f; }
+// The logits of a row from `at` on that fill 16 bytes, wherever the row starts; minus infinity behind the last.  (At a row's end the 16 bytes that end with
+// it are loaded, so that there is one load and no branch, and many can be under way.)
+template <typename T>
+struct Some {
+  static constexpr int kN = 16 / sizeof(T);
+  u32x4_t raw;
+  int from, at;
+  __device__ inline Some() {}
+  __device__ inline Some(const T* row, int at_, int vocab) : at(at_) {
+    typedef u32x4_t Any __attribute__((aligned(2)));
+    from = min(at, vocab - kN);
+    if (vocab >= kN) {
+      raw = *reinterpret_cast<const Any*>(row + from);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = i * kN / 4; e < (i + 1) * kN / 4; ++e)
+          if (from + e >= 0) {
+            if constexpr (sizeof(T) == 4) w = __float_as_uint(row[from + e]);
+            else w |= (uint32_t)row[from + e].bits << (16 * (e & 1));
+          }
+        raw[i] = w;
+      }
+    }
+  }
+  __device__ inline int index(int e) const { return from + e; }
+  __device__ inline float operator[](int e) const {
+    float v;
+    if constexpr (sizeof(T) == 4) {
+      const uint32_t w = raw[e];
+      v = __uint_as_float(w);
+    } else {
+      const uint32_t w = raw[e >> 1];
+      v = to_float(T{(uint16_t)(e & 1 ? w >> 16 : w)});
+    }
+    return from + e >= at ? v + 0.f : -INFINITY;
+  }
+};
 // as unsigned integers these order as the numbers do
 __device__ inline uint32_t order_key(float l) {
   const uint32_t b = __float_as_uint(l);
@@ -109,11 +151,13 @@ __global__ void __launch_bounds__(256) sample_max_kernel(SampleArgs a) {
   __shared__ float scratch[4];
   const int chunk = blockIdx.x, row = blockIdx.y, first = chunk * kChunk;
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
+  constexpr int kN = Some<T>::kN;
   float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kChunk / 256; ++i) {
-    const int at = first + i * 256 + (int)threadIdx.x;
-    if (at < a.vocab) m = fmaxf(m, logit(l, at));
+  for (int i = 0; i < kChunk / 256 / kN; ++i) {
+    const Some<T> x(l, first + (i * 256 + (int)threadIdx.x) * kN, a.vocab);
+#pragma unroll
+    for (int e = 0; e < kN; ++e) m = fmaxf(m, x[e]);
   }
   for (int b = chunk * 256 + (int)threadIdx.x; b < kBins; b += a.chunks * 256) {
     a.mass[(int64_t)row * kBins + b] = 0;
@@ -138,21 +182,21 @@ __global__ void __launch_bounds__(256) sample_bins_kernel(SampleArgs a) {
   __shared__ float scratch[4];
   const int chunk = blockIdx.x, row = blockIdx.y, first = chunk * kChunk;
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
-  float v[kChunk / 256];
+  constexpr int kN = Some<T>::kN;
+  Some<T> x[kChunk / 256 / kN];
+#pragma unroll
+  for (int i = 0; i < kChunk / 256 / kN; ++i) x[i] = Some<T>(l, first + (i * 256 + (int)threadIdx.x) * kN, a.vocab);
+  for (int b = threadIdx.x; b < kBins; b += 256) mass[b] = 0, count[b] = 0;
+  RowSettings s(a, row);
+  s.set_largest(row_max<256>(a, row, scratch));
 #pragma unroll
   for (int i = 0; i < kChunk / 256; ++i) {
-    const int at = first + i * 256 + (int)threadIdx.x;
-    v[i] = at < a.vocab ? logit(l, at) : -INFINITY;
+    const float v = x[i / kN][i % kN];
+    if (!s.valid(v)) continue;
+    const int b = s.bin(v);
+    atomicAdd((unsigned long long*)&mass[b], (unsigned long long)s.mass(v));
+    atomicAdd(&count[b], 1u);
   }
-  for (int b = threadIdx.x; b < kBins; b += 256) mass[b] = 0, count[b] = 0;
-  const RowSettings s(a, row, row_max<256>(a, row, scratch));
-#pragma unroll
-  for (int i = 0; i < kChunk / 256; ++i)
-    if (s.valid(v[i])) {
-      const int b = s.bin(v[i]);
-      atomicAdd((unsigned long long*)&mass[b], (unsigned long long)s.mass(v[i]));
-      atomicAdd(&count[b], 1u);
-    }
   __syncthreads();
   for (int b = threadIdx.x; b < kBins; b += 256) {
     const uint32_t n = count[b];
@@ -204,71 +248,119 @@ struct Place {
 };
 enum PlaceOf { PLACE_OF_COUNT, PLACE_OF_MASS };  // the first token up to and with which the count, or the mass, is the target's
 
-template <int NT>
-struct RowLds {
-  uint64_t mass[kBins];        // running sums of the row's histogram
-  uint32_t count[kBins];
-  union {
-    struct {
-      uint64_t list[kSortMost];  // ~key << 32 | index: sorted ascending these are the tokens in their order
-      uint64_t through[kSortMost];
-    };
-    struct {
-      uint64_t sub_mass[kBins];
-      uint32_t sub_count[kBins];
-    };
-  };
-  uint64_t scratch[2 * NT / 64];
-  float fscratch[NT / 64];
-  uint32_t uscratch[NT / 64];
-  uint32_t n, found, listed;  // listed: the bin in `list`, or kBins
+// The one workgroup that has a row, kRowThreads wide.
+constexpr int kRowThreads = 1024;
+struct BinRange {
+  int first, last;
 };
+constexpr int kRanges = 4;
+struct RowLds {
+  uint64_t mass[kBins];  // running sums of the row's histogram
+  uint32_t count[kBins];
+  uint64_t sub_mass[kBins];
+  uint32_t sub_count[kBins];
+  uint64_t candidate[kCandidates];  // key << 32 | index
+  uint64_t list[kSortMost];         // ~key << 32 | index: sorted ascending these are the tokens in their order
+  uint64_t through[kSortMost];
+  uint64_t scratch[2 * kRowThreads / 64];
+  float fscratch[kRowThreads / 64];
+  uint32_t uscratch[kRowThreads / 64];
+  uint32_t n, found, candidates, chunks_listed;
+  uint16_t chunk[kChunkList];
+  BinRange range[kRanges];
+};
+__device__ inline float key_logit(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 
-// calls f(logit, index) for the valid tokens of bin `b`
-template <typename T, int NT, typename F>
-__device__ inline void for_bin(const SampleArgs& a, const RowSettings& s, const T* l, int row, int b, F&& f) {
-  for (int chunk = 0; chunk < a.chunks; ++chunk) {
-    if (a.mask && !(a.mask[((int64_t)row * a.chunks + chunk) * kMaskWords + (b >> 5)] >> (b & 31) & 1u)) continue;
-    const int end = min(a.vocab, (chunk + 1) * kChunk);
-    for (int i = chunk * kChunk + (int)threadIdx.x; i < end; i += NT) {
-      const float v = logit(l, i);
-      if (s.valid(v) && s.bin(v) == b) f(v, i);
+// Calls f(logit, index) for the valid tokens of the bins of up to kRanges ranges, read from memory.  Of a split row only the chunks that have such tokens are
+// read: their masks are looked at together, and the chunks' tokens then requested as one list.
+template <typename T, typename F>
+__device__ inline void for_ranges(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds& d, const BinRange (&ranges)[kRanges], F&& f) {
+  constexpr int NT = kRowThreads, kN = Some<T>::kN, kParts = kChunk / kN;
+  int least = kBins, most = -1;
+#pragma unroll
+  for (int r = 0; r < kRanges; ++r)
+    if (ranges[r].last >= ranges[r].first) least = min(least, ranges[r].first), most = max(most, ranges[r].last);
+  for (int first = 0; first < a.chunks; first += kChunkList) {
+    int n = min(a.chunks - first, kChunkList);
+    if (a.mask) {
+      __syncthreads();
+      if (threadIdx.x == 0) d.chunks_listed = 0;
+      __syncthreads();
+      for (int c = threadIdx.x; c < n; c += NT) {
+        const uint32_t* const m = a.mask + ((int64_t)row * a.chunks + first + c) * kMaskWords;
+        uint32_t any = 0;
+        for (const BinRange& r : ranges)
+          for (int w = r.first >> 5; w <= r.last >> 5; ++w) {
+            const uint32_t from = w == r.first >> 5 ? ~0u << (r.first & 31) : ~0u, to = w == r.last >> 5 ? ~0u >> (31 - (r.last & 31)) : ~0u;
+            any |= m[w] & from & to;
+          }
+        if (any) d.chunk[atomicAdd(&d.chunks_listed, 1u)] = (uint16_t)c;
+      }
+      __syncthreads();
+      n = (int)d.chunks_listed;
+    }
+    constexpr int kAhead = 4;  // loads under way
+    const int total = n * kParts;
+    for (int i0 = threadIdx.x; i0 < total; i0 += kAhead * NT) {
+      Some<T> x[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int i = min(i0 + q * NT, total - 1), chunk = first + (a.mask ? d.chunk[i / kParts] : i / kParts);
+        x[q] = Some<T>(l, min(chunk * kChunk + i % kParts * kN, a.vocab), a.vocab);
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        if (i0 + q * NT >= total) break;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+          const float v = x[q][e];
+          const int b = s.bin(v);
+          if (b < least || b > most) continue;  // (most tokens end here)
+          bool in = s.valid(v) && b >= ranges[0].first && b <= ranges[0].last;
+#pragma unroll
+          for (int r = 1; r < kRanges; ++r) in |= s.valid(v) && b >= ranges[r].first && b <= ranges[r].last;
+          if (in) f(v, x[q].index(e));
+        }
+      }
     }
   }
 }
+// the same for one range
+template <typename T, typename F>
+__device__ inline void for_bins(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds& d, int b0, int b1, F&& f) {
+  for_ranges(a, s, l, row, d, {{b0, b1}, {0, -1}, {0, -1}, {0, -1}}, f);
+}
 
 // the first of n running sums that reaches the target (the last, if none does); one thread finds it
-template <int NT, typename Reached>
+template <typename Reached>
 __device__ inline int first_reached(int n, uint32_t* found, Reached&& reached) {
   __syncthreads();
   if (threadIdx.x == 0) *found = n - 1;
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += NT)
+  for (int i = threadIdx.x; i < n; i += kRowThreads)
     if (reached(i) && (i == 0 || !reached(i - 1))) *found = i;
   __syncthreads();
   return (int)*found;
 }
 
 // Requires 1 <= target <= the row's count or mass.  (Loops and the list are bounded by themselves, whatever becomes of the logits meanwhile.)
-template <typename T, int NT>
-__device__ inline Place find_place(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds<NT>& d, PlaceOf of, uint64_t target, bool want_index) {
-  const int b = first_reached<NT>(kBins, &d.found, [&](int i) { return (of == PLACE_OF_COUNT ? (uint64_t)d.count[i] : d.mass[i]) >= target; });
+template <typename T>
+__device__ inline Place find_place(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds& d, PlaceOf of, uint64_t target, bool want_index) {
+  constexpr int NT = kRowThreads;
+  const int b = first_reached(kBins, &d.found, [&](int i) { return (of == PLACE_OF_COUNT ? (uint64_t)d.count[i] : d.mass[i]) >= target; });
   uint64_t before_mass = b ? d.mass[b - 1] : 0;
   uint32_t before_count = b ? d.count[b - 1] : 0, n = d.count[b] - before_count;
   uint32_t lo = 0, hi = 0xFFFFFFFFu;  // keys that are left of the bin
   for (int level = 0; n > kSortMost && level < 8; ++level) {
-    __syncthreads();
-    if (threadIdx.x == 0) d.listed = kBins;
     uint32_t least = 0xFFFFFFFFu, most = 0;
-    for_bin<T, NT>(a, s, l, row, b, [&](float v, int) {
+    for_bins(a, s, l, row, d, b, b, [&](float v, int) {
       const uint32_t k = order_key(v);
       if (k >= lo && k <= hi) least = min(least, k), most = max(most, k);
     });
     least = block_reduce<NT>(least, d.uscratch, [](uint32_t x, uint32_t y) { return min(x, y); });
     most = block_reduce<NT>(most, d.uscratch, [](uint32_t x, uint32_t y) { return max(x, y); });
     if (least >= most) {  // all equal: the place is a matter of counting
-      const float v = __uint_as_float(most & 0x80000000u ? most & 0x7FFFFFFFu : ~most);
-      const uint64_t w = s.mass(v);
+      const uint64_t w = s.mass(key_logit(most));
       const uint64_t j = of == PLACE_OF_COUNT ? target - before_count - 1 : (target - before_mass + w - 1) / w - 1;
       Place p{before_mass + (j + 1) * w, w, -1};
       if (want_index) {  // the j-th of them by index: NT tokens at a time, counted in order
@@ -297,16 +389,17 @@ __device__ inline Place find_place(const SampleArgs& a, const RowSettings& s, co
     }
     // cut what is left by the keys' bits, the largest first
     const int shift = max(0, 32 - __clz(most - least) - 10);
+    __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += NT) d.sub_mass[i] = 0, d.sub_count[i] = 0;
     __syncthreads();
-    for_bin<T, NT>(a, s, l, row, b, [&](float v, int) {
+    for_bins(a, s, l, row, d, b, b, [&](float v, int) {
       const uint32_t k = order_key(v);
       if (k < least || k > most) return;
       atomicAdd((unsigned long long*)&d.sub_mass[(most - k) >> shift], (unsigned long long)s.mass(v));
       atomicAdd(&d.sub_count[(most - k) >> shift], 1u);
     });
     running_sums<NT>(d.sub_mass, d.sub_count, d.scratch);
-    const int c = first_reached<NT>(kBins, &d.found, [&](int i) {
+    const int c = first_reached(kBins, &d.found, [&](int i) {
       return (of == PLACE_OF_COUNT ? (uint64_t)before_count + d.sub_count[i] : before_mass + d.sub_mass[i]) >= target;
     });
     hi = most - ((uint32_t)c << shift);
@@ -315,62 +408,166 @@ __device__ inline Place find_place(const SampleArgs& a, const RowSettings& s, co
     const uint32_t skipped_count = c ? d.sub_count[c - 1] : 0;
     n = d.sub_count[c] - skipped_count;
     before_mass += skipped, before_count += skipped_count;
-    __syncthreads();
   }
   n = min(n, (uint32_t)kSortMost);
-  const bool whole = lo == 0 && hi == 0xFFFFFFFFu;
-  if (!whole || d.listed != (uint32_t)b) {
-    int padded = 2;
-    while (padded < (int)n) padded <<= 1;
-    __syncthreads();
-    if (threadIdx.x == 0) d.n = 0, d.listed = whole ? b : kBins;
-    for (int i = (int)n + (int)threadIdx.x; i < padded; i += NT) d.list[i] = ~0ull;
-    __syncthreads();
-    for_bin<T, NT>(a, s, l, row, b, [&](float v, int i) {
-      const uint32_t k = order_key(v);
-      if (k < lo || k > hi) return;
-      const uint32_t at = atomicAdd(&d.n, 1u);
-      if (at < n) d.list[at] = (uint64_t)~k << 32 | (uint32_t)i;
-    });
-    for (int size = 2; size <= padded; size <<= 1)
-      for (int step = size >> 1; step > 0; step >>= 1) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < padded / 2; i += NT) {
-          const int x = 2 * i - (i & (step - 1)), y = x + step;
-          const uint64_t u = d.list[x], v = d.list[y];
-          if ((u > v) == !(x & size)) d.list[x] = v, d.list[y] = u;
-        }
-      }
-    __syncthreads();
-    // running masses: a wave at a time over 64 tokens (the first wave alone, the lists are short)
-    if (threadIdx.x < 64) {
-      uint64_t carry = 0;
-      for (int first = 0; first < (int)n; first += 64) {
-        const int i = first + (int)threadIdx.x;
-        const uint32_t k = ~(uint32_t)(d.list[min(i, (int)n - 1)] >> 32);
-        uint64_t m = i < (int)n ? s.mass(__uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k)) : 0;
+  __syncthreads();
+  if (threadIdx.x == 0) d.n = 0;
+  __syncthreads();
+  for_bins(a, s, l, row, d, b, b, [&](float v, int i) {
+    const uint32_t k = order_key(v);
+    if (k < lo || k > hi) return;
+    const uint32_t at = atomicAdd(&d.n, 1u);
+    if (at < n) d.list[at] = (uint64_t)~k << 32 | (uint32_t)i;
+  });
+  __syncthreads();
+  if (threadIdx.x < 64) {  // each token's place is the number of those before it; then their running masses
+    const bool is = threadIdx.x < n;
+    const uint64_t mine = is ? d.list[threadIdx.x] : ~0ull;
+    int before = 0;
+    for (int i = 0; i < (int)n; ++i) before += __shfl((unsigned long long)mine, i) < mine;
+    if (is) d.list[before] = mine;
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+    const uint64_t sorted = is ? d.list[threadIdx.x] : 0;
+    uint64_t m = is ? s.mass(key_logit(~(uint32_t)(sorted >> 32))) : 0;
 #pragma unroll
-        for (int e = 1; e < 64; e <<= 1) {
-          const uint64_t o = __shfl_up((unsigned long long)m, e);
-          if ((int)threadIdx.x >= e) m += o;
-        }
-        if (i < (int)n) d.through[i] = carry + m;
-        carry += __shfl((unsigned long long)m, 63);
-      }
+    for (int e = 1; e < 64; e <<= 1) {
+      const uint64_t o = __shfl_up((unsigned long long)m, e);
+      if ((int)threadIdx.x >= e) m += o;
     }
+    if (is) d.through[threadIdx.x] = m;
   }
-  const int j = first_reached<NT>((int)n, &d.found, [&](int i) {
+  const int j = first_reached((int)n, &d.found, [&](int i) {
     return (of == PLACE_OF_COUNT ? (uint64_t)before_count + i + 1 : before_mass + d.through[i]) >= target;
   });
   return Place{before_mass + d.through[j], d.through[j] - (j ? d.through[j - 1] : 0), (int)(uint32_t)d.list[j]};
 }
 
+// top-p: the mass that has to be reached; the draw: the one that the drawn token passes
+__device__ inline uint64_t mass_for_p(double top_p, uint64_t mass) {
+  const double p = ceil(fmax(top_p, 0.0) * (double)mass);
+  return min(max((uint64_t)p, (uint64_t)1), mass);
+}
+__device__ inline uint64_t mass_for_u(double u, uint64_t kept) {
+  const double at = u > 0.0 ? u * (double)kept : 0.0;
+  return (at < (double)(kept - 1) ? (uint64_t)at : kept - 1) + 1;
+}
+
+// ---- the same by one wave, over candidates in LDS: no barriers ------------------------------------------------
+__device__ inline void wave_order() {  // a wave's LDS accesses are done in order; this keeps the compiler's order
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+template <typename V, typename Op>
+__device__ inline V wave_reduce(V v, Op op) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v = op(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ inline uint64_t wave_running_sum(uint64_t v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t o = __shfl_up((unsigned long long)v, d);
+    if ((int)(threadIdx.x & 63) >= d) v += o;
+  }
+  return v;
+}
+// the first of the kBins running sums that reaches the target (the last, if none does): of 64 groups of 16, then of one
+template <typename Reached>
+__device__ inline int wave_first_bin(Reached&& reached) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t groups = __ballot(reached(lane * 16 + 15));
+  const int g = groups ? __builtin_ctzll(groups) : 63;
+  const uint64_t bins = __ballot(lane < 16 && reached(g * 16 + (lane & 15)));
+  return g * 16 + (bins ? __builtin_ctzll(bins) : 15);
+}
+// calls f(key, index, is) for the candidates, 64 at a time and in all lanes; `is`: of the bin and between the keys
+template <typename F>
+__device__ inline void for_candidates(const RowSettings& s, const RowLds& d, int b, uint32_t lo, uint32_t hi, F&& f) {
+  const int lane = threadIdx.x & 63, n = (int)d.candidates;
+  for (int first = 0; first < n; first += 64) {
+    const uint64_t c = d.candidate[min(first + lane, n - 1)];
+    const uint32_t k = (uint32_t)(c >> 32);
+    f(k, (uint32_t)c, first + lane < n && k >= lo && k <= hi && s.bin(key_logit(k)) == b);
+  }
+}
+__device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf of, uint64_t target, bool want_index) {
+  const int lane = threadIdx.x & 63;
+  const int b = wave_first_bin([&](int i) { return (of == PLACE_OF_COUNT ? (uint64_t)d.count[i] : d.mass[i]) >= target; });
+  uint64_t before_mass = b ? d.mass[b - 1] : 0;
+  uint32_t before_count = b ? d.count[b - 1] : 0, n = d.count[b] - before_count;
+  uint32_t lo = 0, hi = 0xFFFFFFFFu;
+  for (int level = 0; n > kSortMost && level < 8; ++level) {
+    uint32_t least = 0xFFFFFFFFu, most = 0;
+    for_candidates(s, d, b, lo, hi, [&](uint32_t k, uint32_t, bool is) {
+      if (is) least = min(least, k), most = max(most, k);
+    });
+    least = wave_reduce(least, [](uint32_t x, uint32_t y) { return min(x, y); });
+    most = wave_reduce(most, [](uint32_t x, uint32_t y) { return max(x, y); });
+    if (least >= most) {  // all equal: the place is a matter of counting
+      const uint64_t w = s.mass(key_logit(most));
+      const uint64_t j = of == PLACE_OF_COUNT ? target - before_count - 1 : (target - before_mass + w - 1) / w - 1;
+      Place p{before_mass + (j + 1) * w, w, -1};
+      if (want_index) {  // the least index up to which there are more than j of them, bit by bit
+        uint32_t index = 0;
+        for (int bit = 23; bit >= 0; --bit) {
+          uint64_t below = 0;  // of those with the bits so far and a zero here, and all before them
+          for_candidates(s, d, b, lo, hi, [&](uint32_t, uint32_t i, bool is) { below += __popcll(__ballot(is && i < (index | 1u << bit))); });
+          if (below <= j) index |= 1u << bit;
+        }
+        p.index = (int)index;
+      }
+      return p;
+    }
+    const int shift = max(0, 32 - __clz(most - least) - 6);
+    d.sub_mass[lane] = 0, d.sub_count[lane] = 0;
+    wave_order();
+    for_candidates(s, d, b, least, most, [&](uint32_t k, uint32_t, bool is) {
+      if (!is) return;
+      atomicAdd((unsigned long long*)&d.sub_mass[(most - k) >> shift], (unsigned long long)s.mass(key_logit(k)));
+      atomicAdd(&d.sub_count[(most - k) >> shift], 1u);
+    });
+    wave_order();
+    const uint64_t m = wave_running_sum(d.sub_mass[lane]), c = wave_running_sum(d.sub_count[lane]);
+    const uint64_t at = __ballot((of == PLACE_OF_COUNT ? before_count + c : before_mass + m) >= target);
+    const int i = at ? __builtin_ctzll(at) : 63;
+    hi = most - ((uint32_t)i << shift);
+    lo = max((uint64_t)least, (uint64_t)hi - min((uint64_t)hi, ((uint64_t)1 << shift) - 1));
+    const uint64_t skipped = i ? __shfl((unsigned long long)m, i - 1) : 0, skipped_count = i ? __shfl((unsigned long long)c, i - 1) : 0;
+    n = (uint32_t)(__shfl((unsigned long long)c, i) - skipped_count);
+    before_mass += skipped, before_count += (uint32_t)skipped_count;
+    wave_order();
+  }
+  n = min(n, (uint32_t)kSortMost);
+  int listed = 0;
+  for_candidates(s, d, b, lo, hi, [&](uint32_t k, uint32_t i, bool is) {
+    const uint64_t lanes = __ballot(is);
+    const int at = listed + __popcll(lanes & ((1ull << lane) - 1));
+    if (is && at < (int)n) d.list[at] = (uint64_t)~k << 32 | i;
+    listed += __popcll(lanes);
+  });
+  wave_order();
+  const bool is = lane < (int)n;
+  const uint64_t mine = is ? d.list[lane] : ~0ull;
+  int before = 0;
+  for (int i = 0; i < (int)n; ++i) before += __shfl((unsigned long long)mine, i) < mine;
+  wave_order();
+  if (is) d.list[before] = mine;
+  wave_order();
+  const uint64_t sorted = is ? d.list[lane] : 0, own = is ? s.mass(key_logit(~(uint32_t)(sorted >> 32))) : 0, m = wave_running_sum(own);
+  const uint64_t at = __ballot(is && (of == PLACE_OF_COUNT ? (uint64_t)before_count + lane + 1 : before_mass + m) >= target);
+  const int j = at ? __builtin_ctzll(at) : (int)n - 1;
+  wave_order();
+  return Place{before_mass + __shfl((unsigned long long)m, j), __shfl((unsigned long long)own, j), (int)(uint32_t)__shfl((unsigned long long)sorted, j)};
+}
+
 // d.mass and d.count: the row's histogram.  All threads; the first writes the row's answer.
-template <typename T, int NT>
-__device__ inline void draw_row(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds<NT>& d) {
-  if (threadIdx.x == 0) d.listed = kBins;
-  running_sums<NT>(d.mass, d.count, d.scratch);
+template <typename T>
+__device__ inline void draw_row(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds& d) {
+  const bool first_wave = threadIdx.x < 64;
+  running_sums<kRowThreads>(d.mass, d.count, d.scratch);
   const uint32_t n = d.count[kBins - 1];
+  const uint64_t all = d.mass[kBins - 1];
   if (n == 0) {  // nothing to draw
     if (threadIdx.x == 0) {
       a.token[row] = -1;
@@ -378,32 +575,86 @@ __device__ inline void draw_row(const SampleArgs& a, const RowSettings& s, const
     }
     return;
   }
-  uint64_t kept = d.mass[kBins - 1];
-  if (s.top_k > 0 && (uint32_t)s.top_k < n) kept = find_place<T, NT>(a, s, l, row, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
-  const uint64_t after_k = kept;
-  if (s.top_p < 1.0) {
-    const double p = ceil(fmax(s.top_p, 0.0) * (double)after_k);
-    kept = find_place<T, NT>(a, s, l, row, d, PLACE_OF_MASS, min(max((uint64_t)p, (uint64_t)1), after_k), false).through;
+  const bool by_k = s.top_k > 0 && (uint32_t)s.top_k < n, by_p = s.top_p < 1.0;
+  const bool by_min = s.min_p > 0.0 && s.largest < INFINITY && s.rate > 0.0;  // (at an infinite temperature all masses are the largest)
+  const double u = s.u;
+  // mass >= min_p  <=>  logit >= largest + temperature ln(min_p); the border's rounding to fp32 may cross a bin
+  const double border = by_min ? (double)s.largest + log2(fmin(s.min_p, 1.0)) / s.rate : 0.0;
+  auto before = [&](int b) { return b ? d.mass[b - 1] : (uint64_t)0; };
+
+  if (first_wave) {  // The bins that the places can be in: what is kept is known to within a bin at each cut.
+    BinRange ranges[kRanges] = {{0, -1}, {0, -1}, {0, -1}, {0, -1}};
+    auto bin_of_mass = [&](uint64_t m) { return wave_first_bin([&](int i) { return d.mass[i] >= m; }); };
+    uint64_t low = all, high = all;
+    if (by_k) {
+      const int b = wave_first_bin([&](int i) { return d.count[i] >= (uint32_t)s.top_k; });
+      ranges[0] = {b, b}, low = max(before(b), (uint64_t)1), high = d.mass[b];
+    }
+    if (by_p) {
+      const int b0 = bin_of_mass(mass_for_p(s.top_p, low)), b1 = low == high ? b0 : bin_of_mass(mass_for_p(s.top_p, high));
+      ranges[1] = {b0, b1}, low = max(before(b0), (uint64_t)1), high = min(high, d.mass[b1]);
+    }
+    if (by_min) {
+      const int b = s.bin(fminf(fmaxf((float)border, -3.402823466e38f), s.largest));
+      ranges[2] = {max(0, b - 1), min(kBins - 1, b + 1)};
+      low = min(low, max(before(ranges[2].first), (uint64_t)1)), high = min(high, d.mass[ranges[2].last]);
+    }
+    {
+      const int b0 = bin_of_mass(mass_for_u(u, low)), b1 = low == high ? b0 : bin_of_mass(mass_for_u(u, high));
+      ranges[3] = {b0, b1};
+    }
+    if (threadIdx.x == 0) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < kRanges; ++i) {
+        d.range[i] = ranges[i];
+        if (ranges[i].last >= ranges[i].first) most += d.count[ranges[i].last] - (ranges[i].first ? d.count[ranges[i].first - 1] : 0);
+      }
+      d.candidates = most <= 4 * kCandidates ? 0 : kCandidates + 1;  // (ranges may overlap)
+    }
   }
-  if (s.min_p > 0.0 && s.largest < INFINITY && s.rate > 0.0) {  // (at an infinite temperature all masses are the largest)
-    // mass >= min_p  <=>  logit >= largest + temperature ln(min_p)
-    const double border = (double)s.largest + log2(fmin(s.min_p, 1.0)) / s.rate;
-    const float edge = fmaxf((float)border, -3.402823466e38f);
-    const int b = s.bin(fminf(edge, s.largest));
-    // (the bins before that of the border's neighbours are whole; the border's rounding to fp32 may cross a bin)
-    const int first = max(0, b - 1), last = min(kBins - 1, b + 1);
-    uint64_t mass = 0;
-    for (int i = first; i <= last; ++i)
-      if (d.count[i] != (i ? d.count[i - 1] : 0))
-        for_bin<T, NT>(a, s, l, row, i, [&](float v, int) {
-          if ((double)v >= border) mass += s.mass(v);
+  __syncthreads();
+  BinRange ranges[kRanges];
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i) ranges[i] = d.range[i];
+  const bool gather = d.candidates == 0;
+  __syncthreads();
+  if (gather)  // their tokens, unless they are too many
+    for_ranges(a, s, l, row, d, ranges, [&](float v, int i) {
+      const uint32_t at = atomicAdd(&d.candidates, 1u);
+      if (at < kCandidates) d.candidate[at] = (uint64_t)order_key(v) << 32 | (uint32_t)i;
+    });
+  __syncthreads();
+
+  uint64_t kept = all;
+  Place p;
+  if (d.candidates <= kCandidates) {
+    if (!first_wave) return;
+    if (by_k) kept = wave_find_place(s, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
+    if (by_p) kept = wave_find_place(s, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
+    if (by_min) {
+      unsigned long long mass = 0;
+      for (int b = ranges[2].first; b <= ranges[2].last; ++b)
+        for_candidates(s, d, b, 0, 0xFFFFFFFFu, [&](uint32_t k, uint32_t, bool is) {
+          if (is && (double)key_logit(k) >= border) mass += s.mass(key_logit(k));
         });
-    mass = block_reduce<NT>((unsigned long long)mass, (unsigned long long*)d.scratch, [](unsigned long long x, unsigned long long y) { return x + y; });
-    kept = min(kept, max((first ? d.mass[first - 1] : 0) + mass, (uint64_t)1 << s.shift));
+      mass = wave_reduce(mass, [](unsigned long long x, unsigned long long y) { return x + y; });
+      kept = min(kept, max(before(ranges[2].first) + mass, (uint64_t)1 << s.shift));
+    }
+    p = wave_find_place(s, d, PLACE_OF_MASS, mass_for_u(u, kept), true);
+  } else {
+    if (by_k) kept = find_place(a, s, l, row, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
+    if (by_p) kept = find_place(a, s, l, row, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
+    if (by_min) {
+      unsigned long long mass = 0;
+      for_bins(a, s, l, row, d, ranges[2].first, ranges[2].last, [&](float v, int) {
+        if ((double)v >= border) mass += s.mass(v);
+      });
+      mass = block_reduce<kRowThreads>(mass, (unsigned long long*)d.scratch, [](unsigned long long x, unsigned long long y) { return x + y; });
+      kept = min(kept, max(before(ranges[2].first) + mass, (uint64_t)1 << s.shift));
+    }
+    p = find_place(a, s, l, row, d, PLACE_OF_MASS, mass_for_u(u, kept), true);
   }
-  const double u = (double)a.u[row], at = u > 0.0 ? u * (double)kept : 0.0;
-  const uint64_t target = at < (double)(kept - 1) ? (uint64_t)at : kept - 1;
-  const Place p = find_place<T, NT>(a, s, l, row, d, PLACE_OF_MASS, target + 1, true);
   if (threadIdx.x == 0) {
     a.token[row] = p.index;
     if (a.prob) a.prob[row] = (float)((double)p.mass / (double)kept);
@@ -411,33 +662,47 @@ __device__ inline void draw_row(const SampleArgs& a, const RowSettings& s, const
 }
 
 template <typename T>
-__global__ void __launch_bounds__(512) sample_draw_kernel(SampleArgs a) {
-  __shared__ RowLds<512> d;
+__global__ void __launch_bounds__(kRowThreads) sample_draw_kernel(SampleArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
+  RowLds& d = *reinterpret_cast<RowLds*>(lds_raw);
   const int row = blockIdx.x;
-  for (int b = threadIdx.x; b < kBins; b += 512) d.mass[b] = a.mass[(int64_t)row * kBins + b], d.count[b] = a.count[(int64_t)row * kBins + b];
-  const RowSettings s(a, row, row_max<512>(a, row, d.fscratch));
-  draw_row<T, 512>(a, s, reinterpret_cast<const T*>(a.logits) + row * a.ld, row, d);
+  for (int b = threadIdx.x; b < kBins; b += kRowThreads) d.mass[b] = a.mass[(int64_t)row * kBins + b], d.count[b] = a.count[(int64_t)row * kBins + b];
+  RowSettings s(a, row);
+  s.set_largest(row_max<kRowThreads>(a, row, d.fscratch));
+  draw_row(a, s, reinterpret_cast<const T*>(a.logits) + row * a.ld, row, d);
 }
 
 // A row to a workgroup: all passes.
 template <typename T>
-__global__ void __launch_bounds__(1024) sample_row_kernel(SampleArgs a) {
-  __shared__ RowLds<1024> d;
+__global__ void __launch_bounds__(kRowThreads) sample_row_kernel(SampleArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds_raw[];
+  RowLds& d = *reinterpret_cast<RowLds*>(lds_raw);
   const int row = blockIdx.x;
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
   float m = -INFINITY;
-  for (int i = threadIdx.x; i < a.vocab; i += 1024) m = fmaxf(m, logit(l, i));
-  for (int b = threadIdx.x; b < kBins; b += 1024) d.mass[b] = 0, d.count[b] = 0;
-  const RowSettings s(a, row, block_reduce<1024>(m, d.fscratch, [](float x, float y) { return fmaxf(x, y); }));
-  for (int i = threadIdx.x; i < a.vocab; i += 1024) {
-    const float v = logit(l, i);
-    if (s.valid(v)) {
+  constexpr int kN = Some<T>::kN;
+#pragma unroll 4
+  for (int i = threadIdx.x * kN; i < a.vocab; i += kRowThreads * kN) {
+    const Some<T> x(l, i, a.vocab);
+#pragma unroll
+    for (int e = 0; e < kN; ++e) m = fmaxf(m, x[e]);
+  }
+  for (int b = threadIdx.x; b < kBins; b += kRowThreads) d.mass[b] = 0, d.count[b] = 0;
+  RowSettings s(a, row);
+  s.set_largest(block_reduce<kRowThreads>(m, d.fscratch, [](float x, float y) { return fmaxf(x, y); }));
+#pragma unroll 2
+  for (int i = threadIdx.x * kN; i < a.vocab; i += kRowThreads * kN) {
+    const Some<T> x(l, i, a.vocab);
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+      const float v = x[e];
+      if (!s.valid(v)) continue;
       const int b = s.bin(v);
       atomicAdd((unsigned long long*)&d.mass[b], (unsigned long long)s.mass(v));
       atomicAdd(&d.count[b], 1u);
     }
   }
-  draw_row<T, 1024>(a, s, l, row, d);
+  draw_row(a, s, l, row, d);
 }
 
 // ---- the call ----------------------------------------------------------------------------------------------
@@ -457,15 +722,17 @@ static int check_sample(int rows, int vocab) {
 template <typename T>
 static int launch_sample(const SampleArgs& a, bool split, hipStream_t st) {
   if (!split) {
-    launch_timed(PROF_SELECT, sample_row_kernel<T>, (unsigned)a.rows, 1024, 0, st, a);
+    MDZ_SET_LDS_ONCE(sample_row_kernel<T>, sizeof(RowLds));
+    launch_timed(PROF_SELECT, sample_row_kernel<T>, (unsigned)a.rows, kRowThreads, sizeof(RowLds), st, a);
     MDZ_LAUNCH_CHECK();
     return MDZ_OK;
   }
+  MDZ_SET_LDS_ONCE(sample_draw_kernel<T>, sizeof(RowLds));
   launch_timed(PROF_SELECT, sample_max_kernel<T>, dim3(a.chunks, a.rows), 256, 0, st, a);
   MDZ_LAUNCH_CHECK();
   launch_timed(PROF_SELECT, sample_bins_kernel<T>, dim3(a.chunks, a.rows), 256, 0, st, a);
   MDZ_LAUNCH_CHECK();
-  launch_timed(PROF_SELECT, sample_draw_kernel<T>, (unsigned)a.rows, 512, 0, st, a);
+  launch_timed(PROF_SELECT, sample_draw_kernel<T>, (unsigned)a.rows, kRowThreads, sizeof(RowLds), st, a);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
 }
