@@ -15,11 +15,17 @@ namespace mdz {
 
 constexpr int kBins = 1024;
 constexpr float kBinsPerUnit = 32.f;
-constexpr int kChunk = 4096;      // tokens of a workgroup where a row is split
+constexpr int kChunk = 4096;      // tokens that a workgroup has at a time where a row is split
 constexpr int kSortMost = 64;     // tokens that a wave sorts
 constexpr int kCandidates = 4096;  // tokens of the places' bins in LDS
+constexpr uint32_t kTooMany = 1u << 30;  // (more than a vocabulary has)
 constexpr int kMaskWords = kBins / 32;
 constexpr int kChunkList = 256;   // chunks of a row whose masks are looked at together
+
+struct BinRange {
+  int first, last;
+};
+constexpr int kRanges = 4;
 
 struct SampleArgs {
   const void* logits;
@@ -32,11 +38,16 @@ struct SampleArgs {
   const float* u;
   int32_t* token;
   float* prob;
-  // split rows: per row and chunk the largest logit and which bins it has tokens in; per row the histogram
+  // Split rows.  Per row and chunk the largest logit and which bins it has tokens in; per row the histogram (then its running sums), the bins that its
+  // places can be in, and their tokens.  span: chunks of a workgroup of the second pass.
+  int span;
   float* chunk_max;
   uint32_t* mask;
   uint64_t* mass;
+  uint64_t* candidate;
   uint32_t* count;
+  uint32_t* candidates;
+  BinRange* range;
 };
 
 // a row's settings, and the largest of its logits
@@ -174,34 +185,46 @@ __device__ inline float row_max(const SampleArgs& a, int row, float* scratch) {
   return block_reduce<NT>(m, scratch, [](float x, float y) { return fmaxf(x, y); });
 }
 
-// The chunk's tokens into the row's histogram, through LDS, and which bins they are in.
+// The tokens of a.span chunks into the row's histogram, through LDS, and which bins they are in.  A chunk is requested while the one before it is
+// counted.
 template <typename T>
 __global__ void __launch_bounds__(256) sample_bins_kernel(SampleArgs a) {
   __shared__ uint64_t mass[kBins];
   __shared__ uint32_t count[kBins];
   __shared__ float scratch[4];
-  const int chunk = blockIdx.x, row = blockIdx.y, first = chunk * kChunk;
+  const int row = blockIdx.y, chunk0 = blockIdx.x * a.span, chunks = min(a.span, a.chunks - chunk0);
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
-  constexpr int kN = Some<T>::kN;
-  Some<T> x[kChunk / 256 / kN];
+  constexpr int kN = Some<T>::kN, kLoads = kChunk / 256 / kN;
+  Some<T> x[kLoads];
+  auto load = [&](int chunk) {
 #pragma unroll
-  for (int i = 0; i < kChunk / 256 / kN; ++i) x[i] = Some<T>(l, first + (i * 256 + (int)threadIdx.x) * kN, a.vocab);
+    for (int i = 0; i < kLoads; ++i) x[i] = Some<T>(l, min(chunk * kChunk + (i * 256 + (int)threadIdx.x) * kN, a.vocab), a.vocab);
+  };
+  load(chunk0);
   for (int b = threadIdx.x; b < kBins; b += 256) mass[b] = 0, count[b] = 0;
   RowSettings s(a, row);
   s.set_largest(row_max<256>(a, row, scratch));
+  for (int c = 0; c < chunks; ++c) {
+    Some<T> now[kLoads];
 #pragma unroll
-  for (int i = 0; i < kChunk / 256; ++i) {
-    const float v = x[i / kN][i % kN];
-    if (!s.valid(v)) continue;
-    const int b = s.bin(v);
-    atomicAdd((unsigned long long*)&mass[b], (unsigned long long)s.mass(v));
-    atomicAdd(&count[b], 1u);
+    for (int i = 0; i < kLoads; ++i) now[i] = x[i];
+    if (c + 1 < chunks) load(chunk0 + c + 1);
+#pragma unroll
+    for (int i = 0; i < kChunk / 256; ++i) {
+      const float v = now[i / kN][i % kN];
+      if (!s.valid(v)) continue;
+      const int b = s.bin(v);
+      atomicAdd((unsigned long long*)&mass[b], (unsigned long long)s.mass(v));
+      atomicAdd(&count[b], 1u);
+    }
   }
   __syncthreads();
   for (int b = threadIdx.x; b < kBins; b += 256) {
     const uint32_t n = count[b];
     const uint64_t lanes = __ballot(n != 0);  // 64 bins: two words of the mask
-    if ((threadIdx.x & 31) == 0) a.mask[((int64_t)row * a.chunks + chunk) * kMaskWords + (b >> 5)] = (uint32_t)(lanes >> (threadIdx.x & 32));
+    if ((threadIdx.x & 31) == 0)
+      for (int c = 0; c < chunks; ++c)
+        a.mask[((int64_t)row * a.chunks + chunk0 + c) * kMaskWords + (b >> 5)] = (uint32_t)(lanes >> (threadIdx.x & 32));
     if (n != 0) {
       atomicAdd((unsigned long long*)&a.mass[(int64_t)row * kBins + b], (unsigned long long)mass[b]);
       atomicAdd(&a.count[(int64_t)row * kBins + b], n);
@@ -250,10 +273,6 @@ enum PlaceOf { PLACE_OF_COUNT, PLACE_OF_MASS };  // the first token up to and wi
 
 // The one workgroup that has a row, kRowThreads wide.
 constexpr int kRowThreads = 1024;
-struct BinRange {
-  int first, last;
-};
-constexpr int kRanges = 4;
 struct RowLds {
   uint64_t mass[kBins];  // running sums of the row's histogram
   uint32_t count[kBins];
@@ -316,10 +335,10 @@ __device__ inline void for_ranges(const SampleArgs& a, const RowSettings& s, con
           const float v = x[q][e];
           const int b = s.bin(v);
           if (b < least || b > most) continue;  // (most tokens end here)
-          bool in = s.valid(v) && b >= ranges[0].first && b <= ranges[0].last;
+          bool in = false;
 #pragma unroll
-          for (int r = 1; r < kRanges; ++r) in |= s.valid(v) && b >= ranges[r].first && b <= ranges[r].last;
-          if (in) f(v, x[q].index(e));
+          for (int r = 0; r < kRanges; ++r) in |= b >= ranges[r].first && b <= ranges[r].last;
+          if (in && s.valid(v)) f(v, x[q].index(e));
         }
       }
     }
@@ -481,14 +500,14 @@ __device__ inline int wave_first_bin(Reached&& reached) {
   const uint64_t bins = __ballot(lane < 16 && reached(g * 16 + (lane & 15)));
   return g * 16 + (bins ? __builtin_ctzll(bins) : 15);
 }
-// calls f(key, index, is) for the candidates, 64 at a time and in all lanes; `is`: of the bin and between the keys
+// calls f(key, index, is) for the candidates, 64 at a time and in all lanes; `is`: of the bins and between the keys
 template <typename F>
-__device__ inline void for_candidates(const RowSettings& s, const RowLds& d, int b, uint32_t lo, uint32_t hi, F&& f) {
+__device__ inline void for_candidates(const RowSettings& s, const RowLds& d, int b0, int b1, uint32_t lo, uint32_t hi, F&& f) {
   const int lane = threadIdx.x & 63, n = (int)d.candidates;
   for (int first = 0; first < n; first += 64) {
     const uint64_t c = d.candidate[min(first + lane, n - 1)];
     const uint32_t k = (uint32_t)(c >> 32);
-    f(k, (uint32_t)c, first + lane < n && k >= lo && k <= hi && s.bin(key_logit(k)) == b);
+    f(k, (uint32_t)c, first + lane < n && k >= lo && k <= hi && b0 <= s.bin(key_logit(k)) && s.bin(key_logit(k)) <= b1);
   }
 }
 __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf of, uint64_t target, bool want_index) {
@@ -499,7 +518,7 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
   uint32_t lo = 0, hi = 0xFFFFFFFFu;
   for (int level = 0; n > kSortMost && level < 8; ++level) {
     uint32_t least = 0xFFFFFFFFu, most = 0;
-    for_candidates(s, d, b, lo, hi, [&](uint32_t k, uint32_t, bool is) {
+    for_candidates(s, d, b, b, lo, hi, [&](uint32_t k, uint32_t, bool is) {
       if (is) least = min(least, k), most = max(most, k);
     });
     least = wave_reduce(least, [](uint32_t x, uint32_t y) { return min(x, y); });
@@ -512,7 +531,7 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
         uint32_t index = 0;
         for (int bit = 23; bit >= 0; --bit) {
           uint64_t below = 0;  // of those with the bits so far and a zero here, and all before them
-          for_candidates(s, d, b, lo, hi, [&](uint32_t, uint32_t i, bool is) { below += __popcll(__ballot(is && i < (index | 1u << bit))); });
+          for_candidates(s, d, b, b, lo, hi, [&](uint32_t, uint32_t i, bool is) { below += __popcll(__ballot(is && i < (index | 1u << bit))); });
           if (below <= j) index |= 1u << bit;
         }
         p.index = (int)index;
@@ -522,7 +541,7 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
     const int shift = max(0, 32 - __clz(most - least) - 6);
     d.sub_mass[lane] = 0, d.sub_count[lane] = 0;
     wave_order();
-    for_candidates(s, d, b, least, most, [&](uint32_t k, uint32_t, bool is) {
+    for_candidates(s, d, b, b, least, most, [&](uint32_t k, uint32_t, bool is) {
       if (!is) return;
       atomicAdd((unsigned long long*)&d.sub_mass[(most - k) >> shift], (unsigned long long)s.mass(key_logit(k)));
       atomicAdd(&d.sub_count[(most - k) >> shift], 1u);
@@ -540,7 +559,7 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
   }
   n = min(n, (uint32_t)kSortMost);
   int listed = 0;
-  for_candidates(s, d, b, lo, hi, [&](uint32_t k, uint32_t i, bool is) {
+  for_candidates(s, d, b, b, lo, hi, [&](uint32_t k, uint32_t i, bool is) {
     const uint64_t lanes = __ballot(is);
     const int at = listed + __popcll(lanes & ((1ull << lane) - 1));
     if (is && at < (int)n) d.list[at] = (uint64_t)~k << 32 | i;
@@ -550,7 +569,10 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
   const bool is = lane < (int)n;
   const uint64_t mine = is ? d.list[lane] : ~0ull;
   int before = 0;
-  for (int i = 0; i < (int)n; ++i) before += __shfl((unsigned long long)mine, i) < mine;
+  for (int i = 0; i < (int)n; ++i) {
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), i), low = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+    before += ((uint64_t)high << 32 | low) < mine;
+  }
   wave_order();
   if (is) d.list[before] = mine;
   wave_order();
@@ -561,104 +583,181 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
   return Place{before_mass + __shfl((unsigned long long)m, j), __shfl((unsigned long long)own, j), (int)(uint32_t)__shfl((unsigned long long)sorted, j)};
 }
 
-// d.mass and d.count: the row's histogram.  All threads; the first writes the row's answer.
+// ---- a row from its histogram to its token -----------------------------------------------------------------
+// which cuts a row has, and the logit from which on tokens pass min-p: mass >= min_p  <=>  logit >= largest + temperature ln(min_p)
+struct Cuts {
+  bool by_k, by_p, by_min;
+  double border;
+  __device__ inline Cuts(const RowSettings& s, uint32_t tokens) {
+    by_k = s.top_k > 0 && (uint32_t)s.top_k < tokens, by_p = s.top_p < 1.0;
+    by_min = s.min_p > 0.0 && s.largest < INFINITY && s.rate > 0.0;  // (at an infinite temperature all masses are the largest)
+    border = by_min ? (double)s.largest + log2(fmin(s.min_p, 1.0)) / s.rate : 0.0;
+  }
+};
+
+// One wave, from the histogram's running sums: the bins that the places can be in, what is kept being known to within a bin at each cut.  Returns how many
+// tokens they hold (ranges may overlap: at most).
+__device__ inline uint32_t find_ranges(const RowSettings& s, const Cuts& cuts, const uint64_t* mass, const uint32_t* count, BinRange (&ranges)[kRanges]) {
+  const uint64_t all = mass[kBins - 1];
+  auto before = [&](int b) { return b ? mass[b - 1] : (uint64_t)0; };
+  auto bin_of_mass = [&](uint64_t m) { return wave_first_bin([&](int i) { return mass[i] >= m; }); };
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i) ranges[i] = BinRange{0, -1};
+  uint64_t low = all, high = all;
+  if (cuts.by_k) {
+    const int b = wave_first_bin([&](int i) { return count[i] >= (uint32_t)s.top_k; });
+    ranges[0] = {b, b}, low = max(before(b), (uint64_t)1), high = mass[b];
+  }
+  if (cuts.by_p) {
+    const int b0 = bin_of_mass(mass_for_p(s.top_p, low)), b1 = low == high ? b0 : bin_of_mass(mass_for_p(s.top_p, high));
+    ranges[1] = {b0, b1}, low = max(before(b0), (uint64_t)1), high = min(high, mass[b1]);
+  }
+  if (cuts.by_min) {  // (the border's rounding to fp32 may cross a bin)
+    const int b = s.bin(fminf(fmaxf((float)cuts.border, -3.402823466e38f), s.largest));
+    ranges[2] = {max(0, b - 1), min(kBins - 1, b + 1)};
+    low = min(low, max(before(ranges[2].first), (uint64_t)1)), high = min(high, mass[ranges[2].last]);
+  }
+  const int b0 = bin_of_mass(mass_for_u(s.u, low)), b1 = low == high ? b0 : bin_of_mass(mass_for_u(s.u, high));
+  ranges[3] = {b0, b1};
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i)
+    if (ranges[i].last >= ranges[i].first) most += count[ranges[i].last] - (ranges[i].first ? count[ranges[i].first - 1] : 0);
+  return most;
+}
+__device__ inline bool in_ranges(const BinRange (&ranges)[kRanges], int b) {
+  bool in = false;
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i) in |= b >= ranges[i].first && b <= ranges[i].last;
+  return in;
+}
+
+// d: the running sums and, if they are no more than kCandidates, the candidates.  All threads; the first writes the row's answer.
 template <typename T>
-__device__ inline void draw_row(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds& d) {
-  const bool first_wave = threadIdx.x < 64;
-  running_sums<kRowThreads>(d.mass, d.count, d.scratch);
-  const uint32_t n = d.count[kBins - 1];
-  const uint64_t all = d.mass[kBins - 1];
-  if (n == 0) {  // nothing to draw
-    if (threadIdx.x == 0) {
-      a.token[row] = -1;
-      if (a.prob) a.prob[row] = 0.f;
-    }
-    return;
-  }
-  const bool by_k = s.top_k > 0 && (uint32_t)s.top_k < n, by_p = s.top_p < 1.0;
-  const bool by_min = s.min_p > 0.0 && s.largest < INFINITY && s.rate > 0.0;  // (at an infinite temperature all masses are the largest)
-  const double u = s.u;
-  // mass >= min_p  <=>  logit >= largest + temperature ln(min_p); the border's rounding to fp32 may cross a bin
-  const double border = by_min ? (double)s.largest + log2(fmin(s.min_p, 1.0)) / s.rate : 0.0;
-  auto before = [&](int b) { return b ? d.mass[b - 1] : (uint64_t)0; };
-
-  if (first_wave) {  // The bins that the places can be in: what is kept is known to within a bin at each cut.
-    BinRange ranges[kRanges] = {{0, -1}, {0, -1}, {0, -1}, {0, -1}};
-    auto bin_of_mass = [&](uint64_t m) { return wave_first_bin([&](int i) { return d.mass[i] >= m; }); };
-    uint64_t low = all, high = all;
-    if (by_k) {
-      const int b = wave_first_bin([&](int i) { return d.count[i] >= (uint32_t)s.top_k; });
-      ranges[0] = {b, b}, low = max(before(b), (uint64_t)1), high = d.mass[b];
-    }
-    if (by_p) {
-      const int b0 = bin_of_mass(mass_for_p(s.top_p, low)), b1 = low == high ? b0 : bin_of_mass(mass_for_p(s.top_p, high));
-      ranges[1] = {b0, b1}, low = max(before(b0), (uint64_t)1), high = min(high, d.mass[b1]);
-    }
-    if (by_min) {
-      const int b = s.bin(fminf(fmaxf((float)border, -3.402823466e38f), s.largest));
-      ranges[2] = {max(0, b - 1), min(kBins - 1, b + 1)};
-      low = min(low, max(before(ranges[2].first), (uint64_t)1)), high = min(high, d.mass[ranges[2].last]);
-    }
-    {
-      const int b0 = bin_of_mass(mass_for_u(u, low)), b1 = low == high ? b0 : bin_of_mass(mass_for_u(u, high));
-      ranges[3] = {b0, b1};
-    }
-    if (threadIdx.x == 0) {
-      uint32_t most = 0;
-#pragma unroll
-      for (int i = 0; i < kRanges; ++i) {
-        d.range[i] = ranges[i];
-        if (ranges[i].last >= ranges[i].first) most += d.count[ranges[i].last] - (ranges[i].first ? d.count[ranges[i].first - 1] : 0);
-      }
-      d.candidates = most <= 4 * kCandidates ? 0 : kCandidates + 1;  // (ranges may overlap)
-    }
-  }
-  __syncthreads();
-  BinRange ranges[kRanges];
-#pragma unroll
-  for (int i = 0; i < kRanges; ++i) ranges[i] = d.range[i];
-  const bool gather = d.candidates == 0;
-  __syncthreads();
-  if (gather)  // their tokens, unless they are too many
-    for_ranges(a, s, l, row, d, ranges, [&](float v, int i) {
-      const uint32_t at = atomicAdd(&d.candidates, 1u);
-      if (at < kCandidates) d.candidate[at] = (uint64_t)order_key(v) << 32 | (uint32_t)i;
-    });
-  __syncthreads();
-
-  uint64_t kept = all;
+__device__ inline void settle_row(const SampleArgs& a, const RowSettings& s, const T* l, int row, RowLds& d, const BinRange& min_range) {
+  const Cuts cuts(s, d.count[kBins - 1]);
+  const uint64_t before_min = min_range.first > 0 ? d.mass[min_range.first - 1] : 0;
+  uint64_t kept = d.mass[kBins - 1];
   Place p;
   if (d.candidates <= kCandidates) {
-    if (!first_wave) return;
-    if (by_k) kept = wave_find_place(s, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
-    if (by_p) kept = wave_find_place(s, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
-    if (by_min) {
+    if (threadIdx.x >= 64) return;
+    if (cuts.by_k) kept = wave_find_place(s, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
+    if (cuts.by_p) kept = wave_find_place(s, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
+    if (cuts.by_min) {
       unsigned long long mass = 0;
-      for (int b = ranges[2].first; b <= ranges[2].last; ++b)
-        for_candidates(s, d, b, 0, 0xFFFFFFFFu, [&](uint32_t k, uint32_t, bool is) {
-          if (is && (double)key_logit(k) >= border) mass += s.mass(key_logit(k));
-        });
+      for_candidates(s, d, min_range.first, min_range.last, 0, 0xFFFFFFFFu, [&](uint32_t k, uint32_t, bool is) {
+        if (is && (double)key_logit(k) >= cuts.border) mass += s.mass(key_logit(k));
+      });
       mass = wave_reduce(mass, [](unsigned long long x, unsigned long long y) { return x + y; });
-      kept = min(kept, max(before(ranges[2].first) + mass, (uint64_t)1 << s.shift));
+      kept = min(kept, max(before_min + mass, (uint64_t)1 << s.shift));
     }
-    p = wave_find_place(s, d, PLACE_OF_MASS, mass_for_u(u, kept), true);
+    p = wave_find_place(s, d, PLACE_OF_MASS, mass_for_u(s.u, kept), true);
   } else {
-    if (by_k) kept = find_place(a, s, l, row, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
-    if (by_p) kept = find_place(a, s, l, row, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
-    if (by_min) {
+    if (cuts.by_k) kept = find_place(a, s, l, row, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
+    if (cuts.by_p) kept = find_place(a, s, l, row, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
+    if (cuts.by_min) {
       unsigned long long mass = 0;
-      for_bins(a, s, l, row, d, ranges[2].first, ranges[2].last, [&](float v, int) {
-        if ((double)v >= border) mass += s.mass(v);
+      for_bins(a, s, l, row, d, min_range.first, min_range.last, [&](float v, int) {
+        if ((double)v >= cuts.border) mass += s.mass(v);
       });
       mass = block_reduce<kRowThreads>(mass, (unsigned long long*)d.scratch, [](unsigned long long x, unsigned long long y) { return x + y; });
-      kept = min(kept, max(before(ranges[2].first) + mass, (uint64_t)1 << s.shift));
+      kept = min(kept, max(before_min + mass, (uint64_t)1 << s.shift));
     }
-    p = find_place(a, s, l, row, d, PLACE_OF_MASS, mass_for_u(u, kept), true);
+    p = find_place(a, s, l, row, d, PLACE_OF_MASS, mass_for_u(s.u, kept), true);
   }
   if (threadIdx.x == 0) {
     a.token[row] = p.index;
     if (a.prob) a.prob[row] = (float)((double)p.mass / (double)kept);
   }
+}
+__device__ inline void nothing_to_draw(const SampleArgs& a, int row) {
+  if (threadIdx.x == 0) {
+    a.token[row] = -1;
+    if (a.prob) a.prob[row] = 0.f;
+  }
+}
+
+// Split rows, third pass: a workgroup makes the running sums of a row's histogram and finds its ranges.
+__global__ void __launch_bounds__(256) sample_ranges_kernel(SampleArgs a) {
+  __shared__ uint64_t mass[kBins];
+  __shared__ uint32_t count[kBins];
+  __shared__ uint64_t sums[8];
+  __shared__ float scratch[4];
+  const int row = blockIdx.x;
+  RowSettings s(a, row);
+#pragma unroll
+  for (int i = 0; i < kBins / 256; ++i) {
+    const int b = i * 256 + (int)threadIdx.x;
+    mass[b] = a.mass[(int64_t)row * kBins + b], count[b] = a.count[(int64_t)row * kBins + b];
+  }
+  s.set_largest(row_max<256>(a, row, scratch));
+  running_sums<256>(mass, count, sums);
+#pragma unroll
+  for (int i = 0; i < kBins / 256; ++i) {
+    const int b = i * 256 + (int)threadIdx.x;
+    a.mass[(int64_t)row * kBins + b] = mass[b], a.count[(int64_t)row * kBins + b] = count[b];
+  }
+  if (threadIdx.x >= 64) return;
+  BinRange ranges[kRanges] = {{0, -1}, {0, -1}, {0, -1}, {0, -1}};
+  uint32_t most = 0;
+  if (count[kBins - 1] != 0) most = find_ranges(s, Cuts(s, count[kBins - 1]), mass, count, ranges);
+  if (threadIdx.x == 0) {
+    const bool few = most <= 4 * kCandidates;
+    a.candidates[row] = few ? 0 : kTooMany;  // (then nobody gathers)
+#pragma unroll
+    for (int i = 0; i < kRanges; ++i) a.range[row * kRanges + i] = ranges[i];
+  }
+}
+
+// Fourth pass: a chunk's tokens of the row's ranges to its candidates.
+template <typename T>
+__global__ void __launch_bounds__(256) sample_gather_kernel(SampleArgs a) {
+  __shared__ float scratch[4];
+  __shared__ uint32_t of_wave[4], first;
+  const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
+  const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
+  constexpr int kN = Some<T>::kN, kLoads = kChunk / 256 / kN;
+  if (a.candidates[row] >= kTooMany) return;
+  BinRange ranges[kRanges];
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i) ranges[i] = a.range[row * kRanges + i];
+  Some<T> x[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) x[i] = Some<T>(l, min(chunk * kChunk + (i * 256 + (int)threadIdx.x) * kN, a.vocab), a.vocab);
+  RowSettings s(a, row);
+  s.set_largest(row_max<256>(a, row, scratch));
+  uint32_t mine = 0, is = 0;  // how many of this thread's 16 logits, and which
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+      const float v = x[i][e];
+      const bool in = in_ranges(ranges, s.bin(v)) && s.valid(v);
+      is |= (uint32_t)in << (i * kN + e), mine += in;
+    }
+  uint32_t through = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(through, d);
+    if (lane >= d) through += o;
+  }
+  // (one addition to the row's count per workgroup: they wait for each other; one per wave made 64 flat rows of 128000 take 39 us)
+  if (lane == 63) of_wave[threadIdx.x >> 6] = through;
+  __syncthreads();
+  const uint32_t all = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
+  if (all == 0) return;
+  if (threadIdx.x == 0) first = atomicAdd(&a.candidates[row], all);
+  __syncthreads();
+  uint32_t at = first + through - mine;
+  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += of_wave[w];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+    for (int e = 0; e < kN; ++e)
+      if (is >> (i * kN + e) & 1u) {
+        if (at < kCandidates) a.candidate[(int64_t)row * kCandidates + at] = (uint64_t)order_key(x[i][e]) << 32 | (uint32_t)x[i].index(e);
+        ++at;
+      }
 }
 
 template <typename T>
@@ -667,9 +766,14 @@ __global__ void __launch_bounds__(kRowThreads) sample_draw_kernel(SampleArgs a) 
   RowLds& d = *reinterpret_cast<RowLds*>(lds_raw);
   const int row = blockIdx.x;
   for (int b = threadIdx.x; b < kBins; b += kRowThreads) d.mass[b] = a.mass[(int64_t)row * kBins + b], d.count[b] = a.count[(int64_t)row * kBins + b];
+  const uint32_t candidates = a.candidates[row];
+  if (candidates <= kCandidates)
+    for (uint32_t i = threadIdx.x; i < candidates; i += kRowThreads) d.candidate[i] = a.candidate[(int64_t)row * kCandidates + i];
+  if (threadIdx.x == 0) d.candidates = candidates;
   RowSettings s(a, row);
   s.set_largest(row_max<kRowThreads>(a, row, d.fscratch));
-  draw_row(a, s, reinterpret_cast<const T*>(a.logits) + row * a.ld, row, d);
+  if (d.count[kBins - 1] == 0) return nothing_to_draw(a, row);
+  settle_row(a, s, reinterpret_cast<const T*>(a.logits) + row * a.ld, row, d, a.range[row * kRanges + 2]);
 }
 
 // A row to a workgroup: all passes.
@@ -702,7 +806,30 @@ __global__ void __launch_bounds__(kRowThreads) sample_row_kernel(SampleArgs a) {
       atomicAdd(&d.count[b], 1u);
     }
   }
-  draw_row(a, s, l, row, d);
+  running_sums<kRowThreads>(d.mass, d.count, d.scratch);
+  if (d.count[kBins - 1] == 0) return nothing_to_draw(a, row);
+  if (threadIdx.x < 64) {
+    BinRange ranges[kRanges];
+    const uint32_t most = find_ranges(s, Cuts(s, d.count[kBins - 1]), d.mass, d.count, ranges);
+    if (threadIdx.x == 0) {
+#pragma unroll
+      for (int i = 0; i < kRanges; ++i) d.range[i] = ranges[i];
+      d.candidates = most <= 4 * kCandidates ? 0 : kCandidates + 1;
+    }
+  }
+  __syncthreads();
+  BinRange ranges[kRanges];
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i) ranges[i] = d.range[i];
+  const bool gather = d.candidates == 0;
+  __syncthreads();
+  if (gather)
+    for_ranges(a, s, l, row, d, ranges, [&](float v, int i) {
+      const uint32_t at = atomicAdd(&d.candidates, 1u);
+      if (at < kCandidates) d.candidate[at] = (uint64_t)order_key(v) << 32 | (uint32_t)i;
+    });
+  __syncthreads();
+  settle_row(a, s, l, row, d, ranges[2]);
 }
 
 // ---- the call ----------------------------------------------------------------------------------------------
@@ -711,7 +838,14 @@ static bool sample_splits(int rows, int vocab) { return vocab > 2 * kChunk && ro
 static int64_t sample_bytes(int rows, int vocab) {
   if (!sample_splits(rows, vocab)) return 0;
   const int64_t chunks = (vocab + kChunk - 1) / kChunk;
-  return rows * (kBins * 12 + chunks * (kMaskWords * 4 + 4));
+  return rows * (kBins * 12 + kCandidates * 8 + kRanges * 8 + 4 + chunks * (kMaskWords * 4 + 4));
+}
+// chunks of a workgroup of the second pass
+static int sample_span(int rows, int chunks) {
+#ifdef MDZ_SPAN
+  return MDZ_SPAN;
+#endif
+  return (int64_t)rows * chunks > 4 * num_cus() ? 2 : 1;
 }
 static int check_sample(int rows, int vocab) {
   MDZ_REQUIRE(rows >= 0 && vocab > 0, MDZ_EINVAL, "sample: %d rows of %d logits", rows, vocab);
@@ -730,7 +864,11 @@ static int launch_sample(const SampleArgs& a, bool split, hipStream_t st) {
   MDZ_SET_LDS_ONCE(sample_draw_kernel<T>, sizeof(RowLds));
   launch_timed(PROF_SELECT, sample_max_kernel<T>, dim3(a.chunks, a.rows), 256, 0, st, a);
   MDZ_LAUNCH_CHECK();
-  launch_timed(PROF_SELECT, sample_bins_kernel<T>, dim3(a.chunks, a.rows), 256, 0, st, a);
+  launch_timed(PROF_SELECT, sample_bins_kernel<T>, dim3((a.chunks + a.span - 1) / a.span, a.rows), 256, 0, st, a);
+  MDZ_LAUNCH_CHECK();
+  launch_timed(PROF_SELECT, sample_ranges_kernel, (unsigned)a.rows, 256, 0, st, a);
+  MDZ_LAUNCH_CHECK();
+  launch_timed(PROF_SELECT, sample_gather_kernel<T>, dim3(a.chunks, a.rows), 256, 0, st, a);
   MDZ_LAUNCH_CHECK();
   launch_timed(PROF_SELECT, sample_draw_kernel<T>, (unsigned)a.rows, kRowThreads, sizeof(RowLds), st, a);
   MDZ_LAUNCH_CHECK();
@@ -774,10 +912,12 @@ int medusa_sample(int dtype, const void* logits, int64_t ld, int rows, int vocab
   a.temperature = temperature_opt, a.top_k = top_k_opt, a.top_p = top_p_opt, a.min_p = min_p_opt, a.u = u, a.token = token, a.prob = prob_opt;
   const bool split = need != 0;
   if (split) {
-    a.mass = (uint64_t*)ws;
-    a.count = (uint32_t*)(a.mass + (int64_t)rows * kBins);
-    a.mask = a.count + (int64_t)rows * kBins;
-    a.chunk_max = (float*)(a.mask + (int64_t)rows * a.chunks * kMaskWords);
+    const int64_t n = rows, chunks = a.chunks;
+    a.span = sample_span(rows, a.chunks);
+    a.mass = (uint64_t*)ws, a.candidate = a.mass + n * kBins;
+    a.range = (BinRange*)(a.candidate + n * kCandidates);
+    a.count = (uint32_t*)(a.range + n * kRanges), a.candidates = a.count + n * kBins;
+    a.mask = a.candidates + n, a.chunk_max = (float*)(a.mask + n * chunks * kMaskWords);
   }
   MDZ_WITH_ELEM(dtype, return launch_sample<E>(a, split, (hipStream_t)stream));
 }
