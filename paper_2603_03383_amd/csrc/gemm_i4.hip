@@ -101,6 +101,7 @@ static int pack_i4(int dtype, const I4Source& s, int64_t n_rows, int64_t k, int 
 // its features, then two and four with four waves.  (us at 1 row, one / two / four tiles: 4096 x 4096 5.4 / 6.5 / 8.4; 12288 x 4096 9.1 / 9.7 / 8.9;
 // 128000 x 4096 72.6 / 59.8 / 56.7; 16 rows 12288 x 4096 17.2 / 11.9 / 9.9; gated 688 pairs, one / two: 14.3 / 15.2 at 1 row, 18.3 / 16.8 at 16.)
 // Beyond, the cut of the least modelled time: rounds of workgroups over the chip x turns of a workgroup x a turn's us, measured on full chips.
+constexpr int kMaxGridY = 65535;
 static I4Plan plan_i4(int M, int N, int K, bool gated) {
   const int64_t tiles = i4_tiles(N), blocks = i4_blocks(K), cus = num_cus();
   if (M <= 16) {
@@ -124,6 +125,7 @@ static I4Plan plan_i4(int M, int N, int K, bool gated) {
   for (const Cut& c : kCuts) {
     const int wide = gated ? c.gate_tiles : c.tiles;
     if (M < c.least_rows || M > c.most_rows || wide == 0) continue;
+    if (c.plan.wm == 0 && (M + c.rows - 1) / c.rows > kMaxGridY) continue;  // (its rows are the grid's second axis)
     const int64_t wgs = ((M + c.rows - 1) / c.rows) * ((tiles + wide - 1) / wide), at_once = cus * c.resident;
     const float us = (float)((wgs + at_once - 1) / at_once * ((blocks + c.features - 1) / c.features)) * c.us;
     if (us < least) best = c.plan, least = us;

@@ -842,9 +842,6 @@ static int64_t sample_bytes(int rows, int vocab) {
 }
 // chunks of a workgroup of the second pass
 static int sample_span(int rows, int chunks) {
-#ifdef MDZ_SPAN
-  return MDZ_SPAN;
-#endif
   return (int64_t)rows * chunks > 4 * num_cus() ? 2 : 1;
 }
 static int check_sample(int rows, int vocab) {
