@@ -245,13 +245,31 @@ __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
       *reinterpret_cast<u32x4_t*>(xs + row * 256 + ((r16 ^ (row & 15)) * 16)) = xb[slot][i];
     }
   };
-  // the features behind the last whole block, one by one, and zeros behind them
-  auto put_last_x = [&]() {
-#pragma clang loop unroll(disable)
-    for (int i = 0; i < XR * 8; ++i) {
-      const int row = i >> 1, f = (i & 1) * 64 + lane, k = whole * kI4Block + f;
-      *reinterpret_cast<uint16_t*>(xs + row * 256 + (((f >> 3) ^ (row & 15)) * 16) + (f & 7) * 2) =
-          k < p.K ? *reinterpret_cast<const uint16_t*>(x0 + ((int64_t)min(row, last_row) * p.K + k) * 2) : (uint16_t)0;
+  // the features behind the last whole block, and zeros behind them: each lane loads the 16 bytes from its place on, or where the row ends before, those that
+  // end with it, and moves them down (one load per piece and all under way together: one by one the features of 64 rows took 17 us)
+  auto load_last_x = [&]() {
+    const int k = whole * kI4Block + r16 * 8, at = min(k, p.K - 8);
+#pragma unroll
+    for (int i = 0; i < XR; ++i) {
+      const uint8_t* const row = x0 + (uint32_t)min(i * 4 + q4, last_row) * (uint32_t)(2 * p.K);
+      uint64_t lo = 0, hi = 0;
+      if (at >= 0) {
+        typedef uint64_t Two __attribute__((ext_vector_type(2)));
+        typedef Two AnyTwo __attribute__((aligned(1)));
+        const Two v = *reinterpret_cast<const AnyTwo*>(row + 2 * (int64_t)at);
+        lo = v.x, hi = v.y;
+        const int down = 16 * (k - at);  // bits
+        if (down >= 64) lo = hi >> (down & 63), hi = 0;
+        else if (down > 0) lo = lo >> down | hi << (64 - down), hi >>= down;
+        if (down >= 128) lo = 0;
+      } else {  // fewer than 8 features in all
+        for (int e = 0; k + e < p.K; ++e) {
+          const uint64_t one = reinterpret_cast<const uint16_t*>(row)[k + e];
+          if (e < 4) lo |= one << (16 * e);
+          else hi |= one << (16 * (e - 4));
+        }
+      }
+      xb[0][i] = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
     }
   };
   const I4Constants<E> constants;
@@ -281,7 +299,8 @@ __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
 
   if (hi > whole && lo < hi) {
     stream.load(cb[0], sb[0], zb[0], whole);
-    put_last_x();
+    load_last_x();
+    put_x(0);
     multiply(0);
   }
   if (lo < end) {
