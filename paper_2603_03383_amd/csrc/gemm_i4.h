@@ -9,8 +9,10 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // Codes to 16-bit operands.  A field of four bits at the top of a mantissa, under the exponent of 16, is 16 + q: one mask and one exponent make two
 // operands of a word.  The products are made with 16 + q; what is too much, (16 + z) times the sum of x over the group, is taken off in fp32.  The sums
-// are then some six times larger than with q - z and lose that much in their last bits, 2^-24 relative to them.  (binary16 has a packed
-// subtraction that makes q - z of it, 16 more instructions per tile and block; bf16 has none.)
+// are then some six times larger than with q - z and lose that much in their last bits, 2^-24 relative to them.  binary16 matrices with zero points in
+// groups of 32 or 64 take (16 + q) - (16 + z) instead, which is exact: binary16 has a packed subtraction (bf16 has none), 16 instructions per tile and
+// block in place of one FMA per output and group, and fewer registers (gated 200 x 12800 x 4096 in groups of 64: 94 -> 88 us, of 32: 210 -> 104; of 128
+// it loses, 73 -> 77).
 // The mask and the exponent are kept from the compiler as constants: from registers (w & mask) | magic is one instruction, from literals two.  (No
 // inline assembly for it: the wait between a vector instruction and the MFMA that reads its result is the compiler's to see.)
 constexpr float kI4Offset = 16.f;
@@ -65,17 +67,26 @@ __device__ inline void store_four(T* y, int left, f32x4_t v) {
   }
 }
 
-// of a block: scales of four rows, and their zero points
+// of a block: scales of four rows, and their zero points; or (kI4Subtract) the zero points of the row that a lane's codes are of
 template <int G>
 struct I4Scales {
   uint32_t w[2 * G];
 };
-template <int G>
+template <typename E, int G>
+constexpr bool kI4Subtract = i4_subtracts(__is_same(E, f16_t), G);
+template <typename E, int G>
 struct I4Zeros {
-  uint32_t w[G];
+  static constexpr int kStep = kI4Subtract<E, G> ? G : 4 * G;  // bytes from one to the next
+  typedef std::conditional_t<G == 1, uint8_t, std::conditional_t<G == 2, uint16_t, uint32_t>> Row;
+  uint32_t w[kI4Subtract<E, G> ? 1 : G];
+  __device__ static inline int which(int lane) { return kI4Subtract<E, G> ? lane & 15 : lane >> 4; }
+  __device__ inline void load(const uint8_t* at) {
+    if constexpr (kI4Subtract<E, G>) w[0] = *reinterpret_cast<const Row*>(at);
+    else *this = *reinterpret_cast<const I4Zeros*>(at);
+  }
 };
 // uniform bases of a wave's tiles, and a lane's place in a block
-template <int G, bool ZEROS, bool GATED, int NT>
+template <typename E, int G, bool ZEROS, bool GATED, int NT>
 struct I4Stream {
   static constexpr int kGateTiles = GATED ? NT / 2 : NT;
   const uint8_t* codes[NT];
@@ -91,9 +102,9 @@ struct I4Stream {
       scales[j] = w.scales + at * (32 * G);
       zeros[j] = ZEROS ? w.zeros + at * (16 * G) : nullptr;
     }
-    co = lane * 16, so = (lane >> 4) * (8 * G), zo = (lane >> 4) * (4 * G);
+    co = lane * 16, so = (lane >> 4) * (8 * G), zo = I4Zeros<E, G>::which(lane) * I4Zeros<E, G>::kStep;
   }
-  __device__ inline void load(u32x4_t (&c)[NT], I4Scales<G> (&s)[NT], I4Zeros<G> (&z)[NT], int b) const {
+  __device__ inline void load(u32x4_t (&c)[NT], I4Scales<G> (&s)[NT], I4Zeros<E, G> (&z)[NT], int b) const {
     const int64_t at = __builtin_amdgcn_readfirstlane(b);
     // A block's address is uniform and a lane's place in it 32 bits (kept from the compiler, which would make 64-bit vector addresses of them).
     uint32_t c0 = co, s0 = so, z0 = zo;
@@ -103,9 +114,7 @@ struct I4Stream {
       const u32x4_t* const cp = reinterpret_cast<const u32x4_t*>(codes[j] + at * 1024 + c0);
       c[j] = __builtin_nontemporal_load(cp);
       s[j] = *reinterpret_cast<const I4Scales<G>*>(scales[j] + at * (32 * G) + s0);
-      if constexpr (ZEROS) {
-        z[j] = *reinterpret_cast<const I4Zeros<G>*>(zeros[j] + at * (16 * G) + z0);
-      }
+      if constexpr (ZEROS) z[j].load(zeros[j] + at * (16 * G) + z0);
     }
   }
 };
@@ -114,6 +123,7 @@ struct I4Stream {
 // points start from, or the sums themselves.  x[s][i]: the operands of a block's four steps.
 template <typename E, int G, bool ZEROS, int MT>
 __device__ inline void sum_block(f32x4_t (&c0)[G][MT], const u32x4_t (&x)[4][MT]) {
+  if constexpr (ZEROS && kI4Subtract<E, G>) return;
   constexpr uint32_t kFactor = ZEROS ? I4Elem<E>::kOne : I4Elem<E>::kMinus24;
   const u32x4_t factor{kFactor, kFactor, kFactor, kFactor};
 #pragma unroll
@@ -130,8 +140,9 @@ __device__ inline void sum_block(f32x4_t (&c0)[G][MT], const u32x4_t (&x)[4][MT]
 // tot += the products of one block of features and one tile of columns
 template <typename E, int G, bool ZEROS, int MT>
 __device__ inline void multiply_tile(f32x4_t (&tot)[MT], const u32x4_t (&x)[4][MT], const f32x4_t (&c0)[G][MT], u32x4_t codes, const I4Scales<G>& scales,
-                                     const I4Zeros<G>& zeros, const I4Constants<E>& constants) {
+                                     const I4Zeros<E, G>& zeros, const I4Constants<E>& constants) {
   constexpr int kSteps = 4 / G;  // MFMA steps of a group
+  constexpr bool kSubtract = ZEROS && kI4Subtract<E, G>;
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     f32x4_t acc[MT];
@@ -140,7 +151,13 @@ __device__ inline void multiply_tile(f32x4_t (&tot)[MT], const u32x4_t (&x)[4][M
 #pragma unroll
     for (int s = g * kSteps; s < (g + 1) * kSteps; ++s) {
       const uint32_t word = codes[s];
-      const u32x4_t w = dequantise<E>(word, constants);
+      u32x4_t w = dequantise<E>(word, constants);
+      if constexpr (kSubtract) {
+        typedef _Float16 Eight __attribute__((ext_vector_type(8)));
+        const uint32_t z = 0x4C00u | (zeros.w[0] >> (8 * g) & 0xFFu) << 6;  // 16 + z
+        const uint32_t two = z | z << 16;
+        w = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(Eight, w) - __builtin_bit_cast(Eight, u32x4_t{two, two, two, two}));
+      }
 #pragma unroll
       for (int i = 0; i < MT; ++i) acc[i] = I4Elem<E>::mfma(w, x[s][i], acc[i]);
     }
@@ -148,9 +165,10 @@ __device__ inline void multiply_tile(f32x4_t (&tot)[MT], const u32x4_t (&x)[4][M
     for (int c = 0; c < 4; ++c) {
       const int at = c * G + g;
       const float scale = half_to_float<E>(scales.w[at >> 1], at & 1);
-      const float off = ZEROS ? -kI4Offset - (float)(zeros.w[at >> 2] >> (8 * (at & 3)) & 0xFFu) : 0.f;
+      constexpr bool kTakeOff = ZEROS && !kSubtract;
+      const float off = kTakeOff ? -kI4Offset - (float)(zeros.w[kTakeOff ? at >> 2 : 0] >> (8 * (at & 3)) & 0xFFu) : 0.f;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) tot[i][c] = fmaf(scale, ZEROS ? fmaf(off, c0[g][i].x, acc[i][c]) : acc[i][c], tot[i][c]);
+      for (int i = 0; i < MT; ++i) tot[i][c] = fmaf(scale, kTakeOff ? fmaf(off, c0[g][i].x, acc[i][c]) : acc[i][c], tot[i][c]);
     }
   }
 }
@@ -202,7 +220,7 @@ __device__ inline void finish_i4(const I4Product& p, const f32x4_t (&tot)[NT][MT
 // lines of memory into operands; no wave waits for another before the end.  XR: pieces of four rows that are loaded (4 MT, or fewer).
 template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D, int DX, int WPE>
 __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
-  typedef I4Stream<G, ZEROS, GATED, NT> Stream;
+  typedef I4Stream<E, G, ZEROS, GATED, NT> Stream;
   typedef u32x4_t Any16 __attribute__((aligned(1)));
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds_raw[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -214,7 +232,7 @@ __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
   const Stream stream(p, tile0, lane);
   u32x4_t xb[DX][XR], cb[D][NT];
   I4Scales<G> sb[D][NT];
-  I4Zeros<G> zb[D][NT];
+  I4Zeros<E, G> zb[D][NT];
   uint32_t xo[XR];
 #pragma unroll
   for (int i = 0; i < XR; ++i) xo[i] = (uint32_t)min(i * 4 + q4, last_row) * (uint32_t)(2 * p.K) + r16 * 16;
@@ -439,8 +457,8 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4
       const int mat = GATED && j >= NT / 2, tile = wn * (NT / R::kMats) + (GATED ? j % (NT / 2) : j);
       const uint8_t* const cs = xs + (R::kX + mat * R::kTiles + tile) * 1024 + lane * 16;
       const uint8_t* const ss = xs + (R::kAtScales + mat * R::kScales) * 1024 + tile * (32 * G) + q4 * (8 * G);
-      I4Zeros<G> z{};
-      if constexpr (ZEROS) z = *reinterpret_cast<const I4Zeros<G>*>(xs + (R::kAtZeros + mat * R::kZeros) * 1024 + tile * (16 * G) + q4 * (4 * G));
+      I4Zeros<E, G> z{};
+      if constexpr (ZEROS) z.load(xs + (R::kAtZeros + mat * R::kZeros) * 1024 + tile * (16 * G) + z.which(lane) * z.kStep);
       multiply_tile<E, G, ZEROS>(tot[j], x, c0, *reinterpret_cast<const u32x4_t*>(cs), *reinterpret_cast<const I4Scales<G>*>(ss), z, constants);
     }
 #pragma unroll
@@ -505,8 +523,9 @@ static int launch_i4_rows(I4Product p, hipStream_t st) {
   MDZ_I4_ROWS(4, 4, 1, 8, 1, 2)
 template <typename E, int G, bool ZEROS, bool GATED>
 static int launch_i4_tiles(const I4Product& p, const I4Plan& plan, hipStream_t st) {
+  constexpr int kKind = i4_kind(__is_same(E, f16_t), G, ZEROS);
 #define MDZ_I4_FEW(MT, NT, XR, NW, D, DX, WPE)                                                        \
-  if constexpr (!GATED || NT % 2 == 0)                                                                \
+  if constexpr ((!GATED || NT % 2 == 0) && i4_built(I4Plan{MT, NT, 0, 0, NW, XR}, kKind, GATED))       \
     if (plan.wm == 0 && plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.wk == NW)              \
       return launch_i4_few<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>(p, st);
 #define MDZ_I4_ROWS(MT, NT, WM, WN, WK, WPE) \

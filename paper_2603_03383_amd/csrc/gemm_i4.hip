@@ -98,36 +98,31 @@ static int pack_i4(int dtype, const I4Source& s, int64_t n_rows, int64_t k, int 
 
 // ---- products ----------------------------------------------------------------------------------------
 // Up to 16 rows the weights are the stream and each workgroup of the kernel of few rows takes one column tile (pair) until every CU has one, with eight waves on
-// its features, then two and four with four waves.  (us at 1 row, one / two / four tiles: 4096 x 4096 5.4 / 6.5 / 8.4; 12288 x 4096 9.1 / 9.7 / 8.9;
-// 128000 x 4096 72.6 / 59.8 / 56.7; 16 rows 12288 x 4096 17.2 / 11.9 / 9.9; gated 688 pairs, one / two: 14.3 / 15.2 at 1 row, 18.3 / 16.8 at 16.)
-// Beyond, the cut of the least modelled time: rounds of workgroups over the chip x turns of a workgroup x a turn's us, measured on full chips.
+// its features, then two and four with four waves.  (us at 1 row, one / two / four tiles: 4096 x 4096 5.2 / 6.0 / 8.3; 12288 x 4096 11.8 / 9.5 / 9.0;
+// 22016 x 4096 19.5 / 12.8 / 13.5; 128000 x 4096 72.6 / 59.8 / 56.7; 16 rows 12288 x 4096 17.1 / 11.5 / 10.1; gated 688 pairs, one / two: 12.7 / 14.4 at 1 row,
+// 17.4 / 16.1 at 16.)  In groups of 32 four tiles do not fit the registers (12288 x 4096 at 1 row, two / four: 11.3 / 19.9; with zero points in bf16
+// two tiles with eight / four waves: 17.1 / 20.8).
+// Beyond, the cut of the least modelled time: rounds of workgroups over the chip x turns of a workgroup x a turn's us (kI4Cuts).
 constexpr int kMaxGridY = 65535;
-static I4Plan plan_i4(int M, int N, int K, bool gated) {
+static I4Plan plan_i4(int M, int N, int K, int kind, bool gated) {
   const int64_t tiles = i4_tiles(N), blocks = i4_blocks(K), cus = num_cus();
   if (M <= 16) {
     const int xr = M <= 4 ? 1 : M <= 8 ? 2 : 4;
-    if (gated) return tiles <= cus ? I4Plan{1, 2, 0, 0, 8, xr} : tiles <= 4 * cus && xr < 4 ? I4Plan{1, 2, 0, 0, 4, xr} : I4Plan{1, 4, 0, 0, 4, xr};
-    return tiles <= cus ? I4Plan{1, 1, 0, 0, 8, xr} : tiles <= 2 * cus ? I4Plan{1, 2, 0, 0, 4, xr} : I4Plan{1, 4, 0, 0, 4, xr};
+    const bool of_32 = kind == 2 || kind == 5 || kind == 7;
+    const I4Plan two{1, 2, 0, 0, kind == 5 ? 8 : 4, xr}, four{1, 4, 0, 0, 4, xr};
+    if (gated) return tiles <= cus ? I4Plan{1, 2, 0, 0, 8, xr} : of_32 || (tiles <= 4 * cus && xr < 4) ? two : four;
+    return tiles <= cus ? I4Plan{1, 1, 0, 0, 8, xr} : of_32 || tiles <= 2 * cus ? two : four;
   }
-  struct Cut {
-    I4Plan plan;
-    int least_rows, most_rows, rows, tiles, gate_tiles, features, resident;  // features: blocks of a turn; resident: workgroups of a CU
-    float us;
-  };
-  static constexpr Cut kCuts[] = {
-      {{2, 1, 0, 0, 8, 8}, 17, 32, 32, 1, 0, 8, 1, 1.5f},   {{2, 2, 0, 0, 8, 8}, 17, 32, 32, 2, 1, 8, 1, 2.2f},
-      {{2, 6, 0, 0, 4, 8}, 17, 32, 32, 6, 3, 4, 1, 1.9f},   {{4, 1, 0, 0, 8, 16}, 33, 1 << 30, 64, 1, 0, 8, 1, 2.1f},
-      {{4, 2, 0, 0, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, 1, 2.9f}, {{4, 6, 0, 0, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, 1, 2.7f},
-      {{4, 2, 1, 4, 1, 0}, 17, 1 << 30, 64, 8, 4, 1, 2, 1.5f},  {{4, 4, 1, 8, 1, 0}, 17, 1 << 30, 64, 32, 16, 1, 1, 2.4f},
-  };
   I4Plan best{};
   float least = INFINITY;
-  for (const Cut& c : kCuts) {
+  for (const I4Cut& c : kI4Cuts) {
     const int wide = gated ? c.gate_tiles : c.tiles;
-    if (M < c.least_rows || M > c.most_rows || wide == 0) continue;
+    if (M < c.least_rows || M > c.most_rows || wide == 0 || c.us[kind] == 0.f) continue;
     if (c.plan.wm == 0 && (M + c.rows - 1) / c.rows > kMaxGridY) continue;  // (its rows are the grid's second axis)
-    const int64_t wgs = ((M + c.rows - 1) / c.rows) * ((tiles + wide - 1) / wide), at_once = cus * c.resident;
-    const float us = (float)((wgs + at_once - 1) / at_once * ((blocks + c.features - 1) / c.features)) * c.us;
+    const int64_t wgs = ((int64_t)(M + c.rows - 1) / c.rows) * ((tiles + wide - 1) / wide), at_once = c.us_two[kind] > 0.f ? 2 * cus : cus;
+    const int64_t full = wgs / at_once, rest = wgs % at_once;
+    const float us_full = at_once > cus ? c.us_two[kind] : c.us[kind], us_rest = rest > cus ? us_full : rest > 0 ? c.us[kind] : 0.f;
+    const float us = ((float)full * us_full + us_rest) * (float)((blocks + c.features - 1) / c.features);
     if (us < least) best = c.plan, least = us;
   }
   return best;
@@ -174,7 +169,7 @@ static int product_i4(const char* what, int dtype, const void* x, const void* pa
   const int64_t need = aligned_bytes_i4(M, K);
   MDZ_REQUIRE(ws_bytes >= need && (ws || need == 0), MDZ_EWORKSPACE, "%s: workspace %lld < %lld bytes", what, (long long)ws_bytes, (long long)need);
   MDZ_REQUIRE(need == 0 || (reinterpret_cast<uintptr_t>(ws) & 15) == 0, MDZ_EINVAL, "%s: the workspace must start on 16 bytes", what);
-  const I4Plan plan = plan_i4(M, N, K, second != nullptr);
+  const I4Plan plan = plan_i4(M, N, K, i4_kind(dtype == MDZ_FP16, kI4Block / group, zeros != 0), second != nullptr);
   hipStream_t st = (hipStream_t)stream;
   const bool z = zeros != 0, gated = second != nullptr;
   p.ldx = (int64_t)K * 2;

@@ -57,6 +57,40 @@ struct I4Product {
 struct I4Plan {
   int mt, nt, wm, wn, wk, xr;
 };
+// Whether q - z is made before the products (gemm_i4.h), and what a product costs by: 0 .. 2 groups of 128, 64 and 32 without zero points, 3 .. 5 with them,
+// 6 and 7 groups of 64 and 32 whose zero points are subtracted.
+__host__ __device__ constexpr bool i4_subtracts(bool f16, int groups_of_block) { return f16 && groups_of_block > 1; }
+constexpr int i4_kind(bool f16, int groups_of_block, bool zeros) {
+  const int g = groups_of_block == 1 ? 0 : groups_of_block == 2 ? 1 : 2;
+  return !zeros ? g : i4_subtracts(f16, groups_of_block) ? 5 + g : 3 + g;
+}
+// The cuts for more than 16 rows: for how many rows, rows and tiles (of each matrix, if gated; 0: not gated) of a workgroup, blocks of features of a turn, and a
+// turn's us on a full chip by kind: one workgroup on a CU, and two where two fit (0: they do not).  A us of 0: the kind's registers spill, and other cuts are
+// faster wherever this one would do.
+struct I4Cut {
+  I4Plan plan;
+  int least_rows, most_rows, rows, tiles, gate_tiles, features;
+  float us[8], us_two[8];
+};
+constexpr I4Cut kI4Cuts[] = {
+    {{2, 1, 0, 0, 8, 8}, 17, 32, 32, 1, 0, 8, {1.48f, 1.52f, 1.69f, 1.6f, 1.64f, 1.9f, 1.58f, 1.72f}, {}},
+    {{2, 2, 0, 0, 8, 8}, 17, 32, 32, 2, 1, 8, {2.0f, 2.1f, 2.33f, 2.25f, 2.35f, 2.77f, 2.28f, 2.56f}, {}},
+    {{2, 6, 0, 0, 4, 8}, 17, 32, 32, 6, 3, 4, {2.05f, 2.35f, 3.2f, 2.35f, 3.4f, 4.15f, 3.2f, 3.9f}, {}},
+    {{4, 1, 0, 0, 8, 16}, 33, 1 << 30, 64, 1, 0, 8, {2.55f, 2.6f, 4.0f, 2.7f, 2.95f, 4.05f, 2.62f, 2.75f}, {}},
+    {{4, 2, 0, 0, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, {3.05f, 0.f, 0.f, 3.3f, 0.f, 0.f, 3.17f, 0.f}, {}},
+    {{4, 6, 0, 0, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, {3.05f, 3.7f, 0.f, 3.7f, 0.f, 0.f, 4.0f, 0.f}, {}},
+    {{4, 2, 1, 4, 1, 0}, 17, 1 << 30, 64, 8, 4, 1, {1.03f, 1.04f, 1.15f, 1.1f, 1.22f, 1.55f, 1.07f, 1.28f}, {1.33f, 1.36f, 1.63f, 2.1f, 2.2f, 2.95f, 2.0f, 2.4f}},
+    {{4, 4, 1, 8, 1, 0}, 17, 1 << 30, 64, 32, 16, 1, {2.25f, 2.3f, 2.8f, 2.4f, 3.4f, 3.63f, 2.77f, 3.22f}, {}},
+};
+// Whether the kernel of few rows has this cut for this kind.  Up to 16 rows groups of 32 take two tiles at most, with eight waves where zero points cost registers.
+constexpr bool i4_built(const I4Plan& plan, int kind, bool gated) {
+  const bool of_32 = kind == 2 || kind == 5 || kind == 7;
+  if (plan.mt == 1) return !(of_32 && plan.nt == 4) && !(kind == 5 && plan.nt == 2 && plan.wk == 4) && (gated || kind == 5 || !(plan.nt == 2 && plan.wk == 8));
+  for (const I4Cut& c : kI4Cuts)
+    if (c.plan.wm == 0 && c.plan.mt == plan.mt && c.plan.nt == plan.nt) return c.us[kind] > 0.f;
+  return false;
+}
+
 template <typename E, int G>
 int launch_i4(const I4Product& p, bool zeros, bool gated, const I4Plan& plan, hipStream_t st);
 
