@@ -21,6 +21,8 @@ constexpr int kCandidates = 4096;  // tokens of the places' bins in LDS
 constexpr uint32_t kTooMany = 1u << 30;  // (more than a vocabulary has)
 constexpr int kMaskWords = kBins / 32;
 constexpr int kChunkList = 256;   // chunks of a row whose masks are looked at together
+constexpr int kCounterStep = 32;  // rows' counters of candidates stand in lines of their own: additions to one line wait for each other
+constexpr int kFewCandidates = 256;  // up to here one wave settles a row faster than sixteen with barriers
 
 struct BinRange {
   int first, last;
@@ -583,6 +585,72 @@ __device__ inline Place wave_find_place(const RowSettings& s, RowLds& d, PlaceOf
   return Place{before_mass + __shfl((unsigned long long)m, j), __shfl((unsigned long long)own, j), (int)(uint32_t)__shfl((unsigned long long)sorted, j)};
 }
 
+// ---- the same by all waves, over many candidates in LDS -------------------------------------------------------
+// Calls f(key, index) for the candidates of a bin in the thread that has them.
+template <typename F>
+__device__ inline void block_candidates(const RowSettings& s, const RowLds& d, int b0, int b1, F&& f) {
+  for (int i = threadIdx.x, n = (int)d.candidates; i < n; i += kRowThreads) {
+    const uint64_t c = d.candidate[i];
+    const int b = s.bin(key_logit((uint32_t)(c >> 32)));
+    if (b >= b0 && b <= b1) f((uint32_t)(c >> 32), (uint32_t)c);
+  }
+}
+// The bin is cut once more by the same steps, 1/64 of a bin each; the tokens of the 64th in which the place lies are sorted, by every wave for itself.  (More than
+// a wave has lanes: ties, or nearly; wave_find_place cuts those by their bits.)
+__device__ inline Place block_find_place(const RowSettings& s, RowLds& d, PlaceOf of, uint64_t target, bool want_index) {
+  const int lane = threadIdx.x & 63;
+  const int b = wave_first_bin([&](int i) { return (of == PLACE_OF_COUNT ? (uint64_t)d.count[i] : d.mass[i]) >= target; });
+  uint64_t before_mass = b ? d.mass[b - 1] : 0;
+  uint32_t before_count = b ? d.count[b - 1] : 0;
+  if (threadIdx.x < 64) d.sub_mass[lane] = 0, d.sub_count[lane] = 0;
+  if (threadIdx.x == 0) d.n = 0;
+  __syncthreads();
+  // monotone as the bins are: of the same fp32 number
+  auto part = [&](uint32_t k) { return (int)fmaxf(fminf(((s.top - key_logit(k)) * s.per_unit - (float)b) * 64.f, 63.f), 0.f); };
+  block_candidates(s, d, b, b, [&](uint32_t k, uint32_t) {
+    atomicAdd((unsigned long long*)&d.sub_mass[part(k)], (unsigned long long)s.mass(key_logit(k)));
+    atomicAdd(&d.sub_count[part(k)], 1u);
+  });
+  __syncthreads();
+  const uint64_t sm = wave_running_sum(d.sub_mass[lane]), sc = wave_running_sum(d.sub_count[lane]);
+  const uint64_t reached = __ballot((of == PLACE_OF_COUNT ? before_count + sc : before_mass + sm) >= target);
+  const int i = reached ? __builtin_ctzll(reached) : 63;
+  const uint64_t skipped_mass = i ? __shfl((unsigned long long)sm, i - 1) : 0, skipped = i ? __shfl((unsigned long long)sc, i - 1) : 0;
+  const uint32_t n = (uint32_t)(__shfl((unsigned long long)sc, i) - skipped);
+  if (n > kSortMost) {
+    Place p{0, 0, -1};
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      p = wave_find_place(s, d, of, target, want_index);
+      if (lane == 0) d.through[0] = p.through, d.through[1] = p.mass, d.through[2] = (uint64_t)(uint32_t)p.index;
+    }
+    __syncthreads();
+    p = Place{d.through[0], d.through[1], (int)(uint32_t)d.through[2]};
+    __syncthreads();
+    return p;
+  }
+  before_mass += skipped_mass, before_count += (uint32_t)skipped;
+  block_candidates(s, d, b, b, [&](uint32_t k, uint32_t index) {
+    if (part(k) != i) return;
+    const uint32_t at = atomicAdd(&d.n, 1u);
+    if (at < n) d.list[at] = (uint64_t)~k << 32 | index;
+  });
+  __syncthreads();
+  const bool is = lane < (int)n;
+  const uint64_t mine = is ? d.list[lane] : ~0ull;
+  int before = 0;
+  for (int e = 0; e < (int)n; ++e) {
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), e), low = (uint32_t)__builtin_amdgcn_readlane((int)mine, e);
+    before += ((uint64_t)high << 32 | low) < mine;
+  }
+  const int to = (is ? before : lane) * 4;  // each lane's token to the lane of its place
+  const uint32_t high = (uint32_t)__builtin_amdgcn_ds_permute(to, (int)(mine >> 32)), low = (uint32_t)__builtin_amdgcn_ds_permute(to, (int)mine);
+  const uint64_t own = is ? s.mass(key_logit(~high)) : 0, m = wave_running_sum(own);
+  const uint64_t at = __ballot(is && (of == PLACE_OF_COUNT ? (uint64_t)before_count + lane + 1 : before_mass + m) >= target);
+  const int j = at ? __builtin_ctzll(at) : (int)n - 1;
+  return Place{before_mass + __shfl((unsigned long long)m, j), __shfl((unsigned long long)own, j), __shfl((int)low, j)};
+}
+
 // ---- a row from its histogram to its token -----------------------------------------------------------------
 // which cuts a row has, and the logit from which on tokens pass min-p: mass >= min_p  <=>  logit >= largest + temperature ln(min_p)
 struct Cuts {
@@ -639,7 +707,19 @@ __device__ inline void settle_row(const SampleArgs& a, const RowSettings& s, con
   const uint64_t before_min = min_range.first > 0 ? d.mass[min_range.first - 1] : 0;
   uint64_t kept = d.mass[kBins - 1];
   Place p;
-  if (d.candidates <= kCandidates) {
+  if (d.candidates > kFewCandidates && d.candidates <= kCandidates) {
+    if (cuts.by_k) kept = block_find_place(s, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
+    if (cuts.by_p) kept = block_find_place(s, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
+    if (cuts.by_min) {
+      unsigned long long mass = 0;
+      block_candidates(s, d, min_range.first, min_range.last, [&](uint32_t k, uint32_t) {
+        if ((double)key_logit(k) >= cuts.border) mass += s.mass(key_logit(k));
+      });
+      mass = block_reduce<kRowThreads>(mass, (unsigned long long*)d.scratch, [](unsigned long long x, unsigned long long y) { return x + y; });
+      kept = min(kept, max(before_min + mass, (uint64_t)1 << s.shift));
+    }
+    p = block_find_place(s, d, PLACE_OF_MASS, mass_for_u(s.u, kept), true);
+  } else if (d.candidates <= kCandidates) {
     if (threadIdx.x >= 64) return;
     if (cuts.by_k) kept = wave_find_place(s, d, PLACE_OF_COUNT, (uint64_t)s.top_k, false).through;
     if (cuts.by_p) kept = wave_find_place(s, d, PLACE_OF_MASS, mass_for_p(s.top_p, kept), false).through;
@@ -703,7 +783,7 @@ __global__ void __launch_bounds__(256) sample_ranges_kernel(SampleArgs a) {
   if (count[kBins - 1] != 0) most = find_ranges(s, Cuts(s, count[kBins - 1]), mass, count, ranges);
   if (threadIdx.x == 0) {
     const bool few = most <= 4 * kCandidates;
-    a.candidates[row] = few ? 0 : kTooMany;  // (then nobody gathers)
+    a.candidates[row * kCounterStep] = few ? 0 : kTooMany;  // (then nobody gathers)
 #pragma unroll
     for (int i = 0; i < kRanges; ++i) a.range[row * kRanges + i] = ranges[i];
   }
@@ -717,7 +797,7 @@ __global__ void __launch_bounds__(256) sample_gather_kernel(SampleArgs a) {
   const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
   constexpr int kN = Some<T>::kN, kLoads = kChunk / 256 / kN;
-  if (a.candidates[row] >= kTooMany) return;
+  if (a.candidates[row * kCounterStep] >= kTooMany) return;
   BinRange ranges[kRanges];
 #pragma unroll
   for (int i = 0; i < kRanges; ++i) ranges[i] = a.range[row * kRanges + i];
@@ -746,7 +826,7 @@ __global__ void __launch_bounds__(256) sample_gather_kernel(SampleArgs a) {
   __syncthreads();
   const uint32_t all = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
   if (all == 0) return;
-  if (threadIdx.x == 0) first = atomicAdd(&a.candidates[row], all);
+  if (threadIdx.x == 0) first = atomicAdd(&a.candidates[row * kCounterStep], all);
   __syncthreads();
   uint32_t at = first + through - mine;
   for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += of_wave[w];
@@ -766,7 +846,7 @@ __global__ void __launch_bounds__(kRowThreads) sample_draw_kernel(SampleArgs a) 
   RowLds& d = *reinterpret_cast<RowLds*>(lds_raw);
   const int row = blockIdx.x;
   for (int b = threadIdx.x; b < kBins; b += kRowThreads) d.mass[b] = a.mass[(int64_t)row * kBins + b], d.count[b] = a.count[(int64_t)row * kBins + b];
-  const uint32_t candidates = a.candidates[row];
+  const uint32_t candidates = a.candidates[row * kCounterStep];
   if (candidates <= kCandidates)
     for (uint32_t i = threadIdx.x; i < candidates; i += kRowThreads) d.candidate[i] = a.candidate[(int64_t)row * kCandidates + i];
   if (threadIdx.x == 0) d.candidates = candidates;
@@ -838,7 +918,7 @@ static bool sample_splits(int rows, int vocab) { return vocab > 2 * kChunk && ro
 static int64_t sample_bytes(int rows, int vocab) {
   if (!sample_splits(rows, vocab)) return 0;
   const int64_t chunks = (vocab + kChunk - 1) / kChunk;
-  return rows * (kBins * 12 + kCandidates * 8 + kRanges * 8 + 4 + chunks * (kMaskWords * 4 + 4));
+  return rows * (kBins * 12 + kCandidates * 8 + kRanges * 8 + kCounterStep * 4 + chunks * (kMaskWords * 4 + 4));
 }
 // chunks of a workgroup of the second pass
 static int sample_span(int rows, int chunks) {
@@ -914,7 +994,7 @@ int medusa_sample(int dtype, const void* logits, int64_t ld, int rows, int vocab
     a.mass = (uint64_t*)ws, a.candidate = a.mass + n * kBins;
     a.range = (BinRange*)(a.candidate + n * kCandidates);
     a.count = (uint32_t*)(a.range + n * kRanges), a.candidates = a.count + n * kBins;
-    a.mask = a.candidates + n, a.chunk_max = (float*)(a.mask + n * chunks * kMaskWords);
+    a.mask = a.candidates + n * kCounterStep, a.chunk_max = (float*)(a.mask + n * chunks * kMaskWords);
   }
   MDZ_WITH_ELEM(dtype, return launch_sample<E>(a, split, (hipStream_t)stream));
 }
