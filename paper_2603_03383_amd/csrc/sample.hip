@@ -49,7 +49,8 @@ struct SampleArgs {
   uint64_t* candidate;
   uint32_t* count;
   uint32_t* candidates;
-  BinRange* range;
+  BinRange* range;  // kRanges as find_ranges gives them, then the same without overlaps
+  float* row_max;
 };
 
 // a row's settings, and the largest of its logits
@@ -78,7 +79,10 @@ struct RowSettings {
   // 2^(shift + y), rounded to an integer; 2^f by its series, whose rest behind f^11 is below 7e-15 (the masses' steps are 2^-45 at 128000 tokens)
   __device__ inline uint64_t mass(float l) const {
     const double diff = l == largest ? 0.0 : (double)l - (double)largest;
-    const double y = fmax(diff * rate, -1100.0), n = rint(y), f = y - n;
+    // (added to 1.5 * 2^52 a number is rounded to an integer, which the sum's low bits are)
+    constexpr double kRound = 6755399441055744.0;
+    const double y = fmax(diff * rate, -1000.0), at = y + kRound, f = y - (at - kRound);
+    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, at);
     double e = 4.4455382718708101e-10;
     e = fma(e, f, 7.0549116208011205e-09);
     e = fma(e, f, 1.0178086009239696e-07);
@@ -91,8 +95,9 @@ struct RowSettings {
     e = fma(e, f, 2.4022650695910069e-01);
     e = fma(e, f, 6.9314718055994529e-01);
     e = fma(e, f, 1.0);
-    // added to 2^52 a number is rounded to an integer, which the sum's mantissa is
-    return __builtin_bit_cast(uint64_t, ldexp(e, (int)n + shift) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+    // e * 2^(n + shift) to an integer, as above; -1000 + shift + 1023 is positive
+    const double scale = __builtin_bit_cast(double, (uint64_t)(uint32_t)(n + shift + 1023) << 52);
+    return __builtin_bit_cast(uint64_t, fma(e, scale, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
   }
 };
 
@@ -785,36 +790,66 @@ __global__ void __launch_bounds__(256) sample_ranges_kernel(SampleArgs a) {
     const bool few = most <= 4 * kCandidates;
     a.candidates[row * kCounterStep] = few ? 0 : kTooMany;  // (then nobody gathers)
 #pragma unroll
-    for (int i = 0; i < kRanges; ++i) a.range[row * kRanges + i] = ranges[i];
+    for (int i = 0; i < kRanges; ++i) a.range[row * 2 * kRanges + i] = ranges[i];
+    // ranges that touch become one (what stays over after these rounds is looked at twice, no more)
+#pragma unroll
+    for (int round = 0; round < 2; ++round)
+#pragma unroll
+      for (int i = 0; i < kRanges; ++i)
+#pragma unroll
+        for (int j = i + 1; j < kRanges; ++j) {
+          BinRange &x = ranges[i], &y = ranges[j];
+          if (y.first > y.last || (x.first <= x.last && (x.first > y.last + 1 || y.first > x.last + 1))) continue;
+          x = x.first > x.last ? y : BinRange{min(x.first, y.first), max(x.last, y.last)}, y = {0, -1};
+        }
+#pragma unroll
+    for (int i = 0; i < kRanges; ++i) a.range[row * 2 * kRanges + kRanges + i] = ranges[i];
+    a.row_max[row] = s.largest;
   }
 }
 
 // Fourth pass: a chunk's tokens of the row's ranges to its candidates.
 template <typename T>
 __global__ void __launch_bounds__(256) sample_gather_kernel(SampleArgs a) {
-  __shared__ float scratch[4];
   __shared__ uint32_t of_wave[4], first;
   const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
   constexpr int kN = Some<T>::kN, kLoads = kChunk / 256 / kN;
-  if (a.candidates[row * kCounterStep] >= kTooMany) return;
-  BinRange ranges[kRanges];
-#pragma unroll
-  for (int i = 0; i < kRanges; ++i) ranges[i] = a.range[row * kRanges + i];
   Some<T> x[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) x[i] = Some<T>(l, min(chunk * kChunk + (i * 256 + (int)threadIdx.x) * kN, a.vocab), a.vocab);
+  if (a.candidates[row * kCounterStep] >= kTooMany) return;
+  BinRange ranges[kRanges];
+#pragma unroll
+  for (int i = 0; i < kRanges; ++i) ranges[i] = a.range[row * 2 * kRanges + kRanges + i];
   RowSettings s(a, row);
-  s.set_largest(row_max<256>(a, row, scratch));
-  uint32_t mine = 0, is = 0;  // how many of this thread's 16 logits, and which
+  s.set_largest(a.row_max[row]);
+  uint32_t is = 0;  // which of this thread's 16 logits
+  // A bin is the integer part of (top - logit) * per_unit but for the last one's and for infinities: where neither is near, the ranges' ends are compared with
+  // that, and what cannot be drawn is above all of them, or not a number.
+  bool plain = s.largest < INFINITY && s.per_unit > 0.f;
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i)
+  for (int r = 0; r < kRanges; ++r) plain &= ranges[r].last < kBins - 1;
+  if (plain) {
 #pragma unroll
-    for (int e = 0; e < kN; ++e) {
-      const float v = x[i][e];
-      const bool in = in_ranges(ranges, s.bin(v)) && s.valid(v);
-      is |= (uint32_t)in << (i * kN + e), mine += in;
+    for (int r = 0; r < kRanges; ++r) {
+      if (ranges[r].first > ranges[r].last) continue;
+      const float from = (float)ranges[r].first, to = (float)(ranges[r].last + 1);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+          const float at = (s.top - x[i][e]) * s.per_unit;
+          is |= (uint32_t)(at >= from && at < to) << (i * kN + e);
+        }
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int e = 0; e < kN; ++e) is |= (uint32_t)(in_ranges(ranges, s.bin(x[i][e])) && s.valid(x[i][e])) << (i * kN + e);
+  }
+  const uint32_t mine = __popc(is);
   uint32_t through = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -851,9 +886,10 @@ __global__ void __launch_bounds__(kRowThreads) sample_draw_kernel(SampleArgs a) 
     for (uint32_t i = threadIdx.x; i < candidates; i += kRowThreads) d.candidate[i] = a.candidate[(int64_t)row * kCandidates + i];
   if (threadIdx.x == 0) d.candidates = candidates;
   RowSettings s(a, row);
-  s.set_largest(row_max<kRowThreads>(a, row, d.fscratch));
+  s.set_largest(a.row_max[row]);
+  __syncthreads();
   if (d.count[kBins - 1] == 0) return nothing_to_draw(a, row);
-  settle_row(a, s, reinterpret_cast<const T*>(a.logits) + row * a.ld, row, d, a.range[row * kRanges + 2]);
+  settle_row(a, s, reinterpret_cast<const T*>(a.logits) + row * a.ld, row, d, a.range[row * 2 * kRanges + 2]);
 }
 
 // A row to a workgroup: all passes.
@@ -918,7 +954,7 @@ static bool sample_splits(int rows, int vocab) { return vocab > 2 * kChunk && ro
 static int64_t sample_bytes(int rows, int vocab) {
   if (!sample_splits(rows, vocab)) return 0;
   const int64_t chunks = (vocab + kChunk - 1) / kChunk;
-  return rows * (kBins * 12 + kCandidates * 8 + kRanges * 8 + kCounterStep * 4 + chunks * (kMaskWords * 4 + 4));
+  return rows * (kBins * 12 + kCandidates * 8 + 2 * kRanges * 8 + kCounterStep * 4 + 4 + chunks * (kMaskWords * 4 + 4));
 }
 // chunks of a workgroup of the second pass
 static int sample_span(int rows, int chunks) {
@@ -993,8 +1029,9 @@ int medusa_sample(int dtype, const void* logits, int64_t ld, int rows, int vocab
     a.span = sample_span(rows, a.chunks);
     a.mass = (uint64_t*)ws, a.candidate = a.mass + n * kBins;
     a.range = (BinRange*)(a.candidate + n * kCandidates);
-    a.count = (uint32_t*)(a.range + n * kRanges), a.candidates = a.count + n * kBins;
+    a.count = (uint32_t*)(a.range + n * 2 * kRanges), a.candidates = a.count + n * kBins;
     a.mask = a.candidates + n * kCounterStep, a.chunk_max = (float*)(a.mask + n * chunks * kMaskWords);
+    a.row_max = a.chunk_max + n * chunks;
   }
   MDZ_WITH_ELEM(dtype, return launch_sample<E>(a, split, (hipStream_t)stream));
 }
