@@ -484,10 +484,11 @@ static int launch_i4_few(I4Product p, hipStream_t st) {
 
 template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int WPE>
 static int launch_i4_rows(I4Product p, hipStream_t st) {
-  // (three turns fit but for the widest tiles in groups of 32 with zero points)
-  constexpr int NS = I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, 3>::kLds <= 160 * 1024 ? 3 : 2;
+  // Two turns, so that a CU has two workgroups or three: their phases of loads, LDS reads, conversions and products then overlap.  (One workgroup of eight waves and
+  // three turns, all in step: gated 1024 x 11008 x 4096 219 us where two of four waves take 200, 64 x 128000 x 4096 85 and 81.)
+  constexpr int NS = 2;
   typedef I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, NS> R;
-  static_assert(R::kLds <= 160 * 1024, "LDS of a CU");
+  static_assert(R::kLds <= 80 * 1024, "two workgroups share a CU's LDS");
   p.nb_m = (p.M + R::kRows - 1) / R::kRows, p.nb_n = (p.n_tiles + R::kTiles - 1) / R::kTiles;
   const int64_t workgroups = ((int64_t)p.nb_m * p.nb_n + 7) / 8 * 8;
   MDZ_REQUIRE(workgroups * R::kWaves * 64 <= (int64_t)UINT32_MAX, MDZ_EUNSUPPORTED, "linear_i4: %d x %d outputs are more than one launch takes", p.M, p.N);
@@ -520,7 +521,7 @@ static int launch_i4_rows(I4Product p, hipStream_t st) {
   MDZ_I4_FEW(4, 2, 16, 8, 2, 1, 2)      \
   MDZ_I4_FEW(4, 6, 16, 4, 2, 1, 1)      \
   MDZ_I4_ROWS(4, 2, 1, 4, 1, 2)         \
-  MDZ_I4_ROWS(4, 4, 1, 8, 1, 2)
+  MDZ_I4_ROWS(4, 4, 1, 4, 1, 2)
 template <typename E, int G, bool ZEROS, bool GATED>
 static int launch_i4_tiles(const I4Product& p, const I4Plan& plan, hipStream_t st) {
   constexpr int kKind = i4_kind(__is_same(E, f16_t), G, ZEROS);

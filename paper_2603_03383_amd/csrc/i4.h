@@ -65,7 +65,7 @@ constexpr int i4_kind(bool f16, int groups_of_block, bool zeros) {
   return !zeros ? g : i4_subtracts(f16, groups_of_block) ? 5 + g : 3 + g;
 }
 // The cuts for more than 16 rows: for how many rows, rows and tiles (of each matrix, if gated; 0: not gated) of a workgroup, blocks of features of a turn, and a
-// turn's us on a full chip by kind: one workgroup on a CU, and two where two fit (0: they do not).  A us of 0: the kind's registers spill, and other cuts are
+// turn's us on a full chip by kind: with one workgroup on a CU, and with two (0: the kernel of few rows, one).  A us of 0: the kind's registers spill, and other cuts are
 // faster wherever this one would do.
 struct I4Cut {
   I4Plan plan;
@@ -79,8 +79,8 @@ constexpr I4Cut kI4Cuts[] = {
     {{4, 1, 0, 0, 8, 16}, 33, 1 << 30, 64, 1, 0, 8, {2.55f, 2.6f, 4.0f, 2.7f, 2.95f, 4.05f, 2.62f, 2.75f}, {}},
     {{4, 2, 0, 0, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, {3.05f, 0.f, 0.f, 3.3f, 0.f, 0.f, 3.17f, 0.f}, {}},
     {{4, 6, 0, 0, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, {3.05f, 3.7f, 0.f, 3.7f, 0.f, 0.f, 4.0f, 0.f}, {}},
-    {{4, 2, 1, 4, 1, 0}, 17, 1 << 30, 64, 8, 4, 1, {1.03f, 1.04f, 1.15f, 1.1f, 1.22f, 1.55f, 1.07f, 1.28f}, {1.33f, 1.36f, 1.63f, 2.1f, 2.2f, 2.95f, 2.0f, 2.4f}},
-    {{4, 4, 1, 8, 1, 0}, 17, 1 << 30, 64, 32, 16, 1, {2.25f, 2.3f, 2.8f, 2.4f, 3.4f, 3.63f, 2.77f, 3.22f}, {}},
+    {{4, 2, 1, 4, 1, 0}, 17, 1 << 30, 64, 8, 4, 1, {0.95f, 1.0f, 1.16f, 1.15f, 1.22f, 1.54f, 1.04f, 1.2f}, {1.2f, 1.25f, 1.53f, 1.36f, 1.55f, 2.0f, 1.46f, 1.67f}},
+    {{4, 4, 1, 4, 1, 0}, 17, 1 << 30, 64, 16, 8, 1, {1.38f, 1.43f, 2.05f, 1.55f, 1.85f, 2.43f, 1.69f, 2.07f}, {2.12f, 2.35f, 2.87f, 2.33f, 4.1f, 3.42f, 2.65f, 3.1f}},
 };
 // Whether the kernel of few rows has this cut for this kind.  Up to 16 rows groups of 32 take two tiles at most, with eight waves where zero points cost registers.
 constexpr bool i4_built(const I4Plan& plan, int kind, bool gated) {
