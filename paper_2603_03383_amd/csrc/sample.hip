@@ -6,9 +6,14 @@
 // token up to which p of that lies, min-p the mass of the logits from a border on; the kept tokens are the shortest of these beginnings, and the draw is the
 // token at which the running sum passes u times their mass.  So nothing is sorted but the bin of a histogram in which such a place lies.
 //
-// Bins: 1024 steps of (largest - logit) / temperature, 1/32 each.  A place is found in the bins' running sums; its bin is cut again by the bits of its
-// logits into 1024, until it holds up to 64 tokens, which a wave sorts, or equal ones, which are counted.  Which bins the places of a row can
+// Bins: 1024 steps of (largest - logit) / temperature, 1/32 each.  A place is found in the bins' running sums; its bin is cut again, by 64ths of a bin or by the
+// bits of its logits, until up to 64 tokens are left, which a wave sorts, or equal ones, which are counted.  Which bins the places of a row can
 // lie in follows from the running sums alone, so their tokens are read once, into LDS (up to kCandidates; from memory each time beyond that).
+//
+// What bounds it.  A split row takes five launches that wait for each other: largest logit, histogram, ranges, their tokens, the draw; 1 x 128000 fp32 logits 3.0 + 6.1 +
+// 5.3 + 5.0 + 6.6 us, all latency.  64 x 128000: 7.3 + 19 + 5.7 + 13.8 + 14.1; three passes over the logits, whose 33 MB take 7 us each, in the second the masses
+// (6 us of 64-bit FMAs; with masses of one instruction it takes 12.6; its LDS additions and the sums over workgroups hide behind them, 1-2 us when left out), in the
+// fourth the wait for one addition per workgroup, in the last two passes over some 3000 candidates for each of two places.
 #include "kernels.h"
 
 namespace mdz {
@@ -22,7 +27,9 @@ constexpr uint32_t kTooMany = 1u << 30;  // (more than a vocabulary has)
 constexpr int kMaskWords = kBins / 32;
 constexpr int kChunkList = 256;   // chunks of a row whose masks are looked at together
 constexpr int kCounterStep = 32;  // rows' counters of candidates stand in lines of their own: additions to one line wait for each other
-constexpr int kFewCandidates = 256;  // up to here one wave settles a row faster than sixteen with barriers
+// Up to here one wave settles a row faster than sixteen with barriers (us of a call at 1 x 128000 with 20 / 100 / 200 / 400 / 800 candidates: 24.0 / 25.8 / 27.9 /
+// 31.8 / 38.1 by one wave, 25.6 / 26.0 / 26.7 / 28.0 / 30.1 by sixteen).
+constexpr int kFewCandidates = 128;
 
 struct BinRange {
   int first, last;
