@@ -10,9 +10,9 @@
 // bits of its logits, until up to 64 tokens are left, which a wave sorts, or equal ones, which are counted.  Which bins the places of a row can
 // lie in follows from the running sums alone, so their tokens are read once, into LDS (up to kCandidates; from memory each time beyond that).
 //
-// What bounds it.  A split row takes five launches that wait for each other: largest logit, histogram, ranges, their tokens, the draw; 1 x 128000 fp32 logits 3.0 + 6.1 +
-// 5.3 + 5.0 + 6.6 us, all latency.  64 x 128000: 7.3 + 19 + 5.7 + 13.8 + 14.1; three passes over the logits, whose 33 MB take 7 us each, in the second the masses
-// (6 us of 64-bit FMAs; with masses of one instruction it takes 12.6; its LDS additions and the sums over workgroups hide behind them, 1-2 us when left out), in the
+// What bounds it.  A split row takes five launches that wait for each other: largest logit, histogram, ranges, their tokens, the draw; 1 x 128000 fp32 logits 3.0 + 5.9 +
+// 5.5 + 4.4 + 6.6 us, all latency.  64 x 128000: 7.6 + 18.1 + 5.8 + 11.8 + 14.4; three passes over the logits, whose 33 MB take 7 us each, in the second the masses
+// (6 us of 64-bit arithmetic: with masses of one instruction the pass took 12.6 of then 18.8 us, without sums over workgroups 18.0), in the
 // fourth the wait for one addition per workgroup, in the last two passes over some 3000 candidates for each of two places.
 #include "kernels.h"
 
@@ -85,7 +85,7 @@ struct RowSettings {
   __device__ inline int bin(float l) const { return (int)fmaxf(fminf((top - l) * per_unit, (float)(kBins - 1)), 0.f); }
   // 2^(shift + y), rounded to an integer; 2^f by its series, whose rest behind f^11 is below 7e-15 (the masses' steps are 2^-45 at 128000 tokens)
   __device__ inline uint64_t mass(float l) const {
-    const double diff = l == largest ? 0.0 : (double)l - (double)largest;
+    const double diff = (double)fminf(l, 3.402823466e38f) - (double)top;  // (zero for infinities beside an infinity)
     // (added to 1.5 * 2^52 a number is rounded to an integer, which the sum's low bits are)
     constexpr double kRound = 6755399441055744.0;
     const double y = fmax(diff * rate, -1000.0), at = y + kRound, f = y - (at - kRound);
@@ -139,17 +139,13 @@ struct Some {
     }
   }
   __device__ inline int index(int e) const { return from + e; }
-  __device__ inline float operator[](int e) const {
-    float v;
-    if constexpr (sizeof(T) == 4) {
-      const uint32_t w = raw[e];
-      v = __uint_as_float(w);
-    } else {
-      const uint32_t w = raw[e >> 1];
-      v = to_float(T{(uint16_t)(e & 1 ? w >> 16 : w)});
-    }
-    return from + e >= at ? v + 0.f : -INFINITY;
+  // (where the row is known not to end here)
+  __device__ inline float inside(int e) const {
+    const uint32_t w = raw[sizeof(T) == 4 ? e : e >> 1];
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w) + 0.f;
+    else return to_float(T{(uint16_t)(e & 1 ? w >> 16 : w)}) + 0.f;
   }
+  __device__ inline float operator[](int e) const { return from + e >= at ? inside(e) : -INFINITY; }
 };
 // as unsigned integers these order as the numbers do
 __device__ inline uint32_t order_key(float l) {
@@ -223,14 +219,18 @@ __global__ void __launch_bounds__(256) sample_bins_kernel(SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) now[i] = x[i];
     if (c + 1 < chunks) load(chunk0 + c + 1);
+    auto add = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < kChunk / 256; ++i) {
-      const float v = now[i / kN][i % kN];
-      if (!s.valid(v)) continue;
-      const int b = s.bin(v);
-      atomicAdd((unsigned long long*)&mass[b], (unsigned long long)s.mass(v));
-      atomicAdd(&count[b], 1u);
-    }
+      for (int i = 0; i < kChunk / 256; ++i) {
+        const float v = decltype(whole)::value ? now[i / kN].inside(i % kN) : now[i / kN][i % kN];
+        if (!s.valid(v)) continue;
+        const int b = s.bin(v);
+        atomicAdd((unsigned long long*)&mass[b], (unsigned long long)s.mass(v));
+        atomicAdd(&count[b], 1u);
+      }
+    };
+    if ((chunk0 + c + 1) * kChunk <= a.vocab) add(std::true_type{});
+    else add(std::false_type{});
   }
   __syncthreads();
   for (int b = threadIdx.x; b < kBins; b += 256) {
@@ -819,7 +819,7 @@ __global__ void __launch_bounds__(256) sample_ranges_kernel(SampleArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(256) sample_gather_kernel(SampleArgs a) {
   __shared__ uint32_t of_wave[4], first;
-  const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
+  const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63, first_of_chunk = chunk * kChunk;
   const T* const l = reinterpret_cast<const T*>(a.logits) + row * a.ld;
   constexpr int kN = Some<T>::kN, kLoads = kChunk / 256 / kN;
   Some<T> x[kLoads];
@@ -831,55 +831,48 @@ __global__ void __launch_bounds__(256) sample_gather_kernel(SampleArgs a) {
   for (int i = 0; i < kRanges; ++i) ranges[i] = a.range[row * 2 * kRanges + kRanges + i];
   RowSettings s(a, row);
   s.set_largest(a.row_max[row]);
-  uint32_t is = 0;  // which of this thread's 16 logits
+  constexpr int kOf = kLoads * kN;
+  uint64_t is[kOf];  // which lanes' logits, each logit of a thread
   // A bin is the integer part of (top - logit) * per_unit but for the last one's and for infinities: where neither is near, the ranges' ends are compared with
   // that, and what cannot be drawn is above all of them, or not a number.
-  bool plain = s.largest < INFINITY && s.per_unit > 0.f;
+  bool plain = s.largest < INFINITY && s.per_unit > 0.f && first_of_chunk + kChunk <= a.vocab;
 #pragma unroll
   for (int r = 0; r < kRanges; ++r) plain &= ranges[r].last < kBins - 1;
   if (plain) {
+    float at[kOf];
+#pragma unroll
+    for (int k = 0; k < kOf; ++k) at[k] = (s.top - x[k / kN].inside(k % kN)) * s.per_unit, is[k] = 0;
 #pragma unroll
     for (int r = 0; r < kRanges; ++r) {
       if (ranges[r].first > ranges[r].last) continue;
       const float from = (float)ranges[r].first, to = (float)(ranges[r].last + 1);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-        for (int e = 0; e < kN; ++e) {
-          const float at = (s.top - x[i][e]) * s.per_unit;
-          is |= (uint32_t)(at >= from && at < to) << (i * kN + e);
-        }
+      for (int k = 0; k < kOf; ++k) is[k] |= __ballot(at[k] >= from) & __ballot(at[k] < to);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-      for (int e = 0; e < kN; ++e) is |= (uint32_t)(in_ranges(ranges, s.bin(x[i][e])) && s.valid(x[i][e])) << (i * kN + e);
+    for (int k = 0; k < kOf; ++k) is[k] = __ballot(in_ranges(ranges, s.bin(x[k / kN][k % kN])) && s.valid(x[k / kN][k % kN]));
   }
-  const uint32_t mine = __popc(is);
-  uint32_t through = mine;
+  uint32_t mine = 0;  // of the wave
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_up(through, d);
-    if (lane >= d) through += o;
-  }
+  for (int k = 0; k < kOf; ++k) mine += __popcll(is[k]);
   // (one addition to the row's count per workgroup: they wait for each other; one per wave made 64 flat rows of 128000 take 39 us)
-  if (lane == 63) of_wave[threadIdx.x >> 6] = through;
+  if (lane == 0) of_wave[threadIdx.x >> 6] = mine;
   __syncthreads();
   const uint32_t all = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
   if (all == 0) return;
   if (threadIdx.x == 0) first = atomicAdd(&a.candidates[row * kCounterStep], all);
   __syncthreads();
-  uint32_t at = first + through - mine;
+  uint32_t at = first;
   for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += of_wave[w];
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-    for (int e = 0; e < kN; ++e)
-      if (is >> (i * kN + e) & 1u) {
-        if (at < kCandidates) a.candidate[(int64_t)row * kCandidates + at] = (uint64_t)order_key(x[i][e]) << 32 | (uint32_t)x[i].index(e);
-        ++at;
-      }
+  for (int k = 0; k < kOf; ++k) {
+    if (is[k] == 0) continue;
+    const uint32_t to = at + __popcll(is[k] & ((1ull << lane) - 1));
+    if ((is[k] >> lane & 1) && to < kCandidates)
+      a.candidate[(int64_t)row * kCandidates + to] = (uint64_t)order_key(x[k / kN][k % kN]) << 32 | (uint32_t)x[k / kN].index(k % kN);
+    at += __popcll(is[k]);
+  }
 }
 
 template <typename T>
