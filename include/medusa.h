@@ -297,6 +297,7 @@ int medusa_swiglu_i4(int dtype, const void* x, const void* gate_packed, const vo
  * vocab (at most 2^24), and their sums are exact: a row's token depends on nothing but the row.
  * Drawn at every node of a tree, the tokens take node_argmax's place in accept_longest_prefix: the path is then one that
  * sampling token by token gives with these random numbers, and next_root the token drawn after it.
+ * Outputs must not overlap inputs or each other.
  * ws: medusa_sample_workspace_bytes(rows, vocab) bytes of scratch that start on 16 bytes (0: ws may be NULL); nothing in it has
  * to be set, and nothing is kept in it. */
 int64_t medusa_sample_workspace_bytes(int rows, int vocab);
