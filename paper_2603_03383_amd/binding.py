@@ -423,12 +423,19 @@ def medusa_packed_i4_bytes(n_rows: int, k: int, group: int, zeros: bool = False)
     return _check(lib().medusa_packed_i4_bytes(n_rows, k, group, int(zeros)))
 
 
+def _whole(name: str, t: torch.Tensor, device: int) -> int:
+    """Address of a contiguous tensor on this GPU whose shape and type are known to be right, or free."""
+    if t.get_device() != device or not t.is_contiguous():
+        return _operand(name, t, t.shape, t.dtype, device)
+    return t.data_ptr()
+
+
 def _packed_i4(name: str, t: torch.Tensor, n: int, k: int, group: int, zeros: bool, device: int) -> int:
     """Scales and zero points stand where the codes end: a buffer of other sizes was packed for another matrix."""
-    got, want = t.numel() * t.element_size(), medusa_packed_i4_bytes(n, k, group, bool(zeros))
+    got, want = t.nbytes, medusa_packed_i4_bytes(n, k, group, bool(zeros))
     if got != want:
         raise MedusaError(-2, f"{name}: {got} bytes are not those of [{n}, {k}] in groups of {group}, {want}")
-    return _operand(name, t, t.shape, t.dtype, device)
+    return _whole(name, t, device)
 
 
 def medusa_pack_weight_i4(src: torch.Tensor, group: int, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0, zeros: bool = False, stream=None) -> None:
@@ -463,24 +470,24 @@ def medusa_swiglu_i4_workspace_bytes(M: int, ffn: int, K: int) -> int:
 def medusa_linear_i4(x: torch.Tensor, packed: torch.Tensor, group: int, zeros: bool, y: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """y [M, N] (any storage dtype) = x [M, K] (bf16 or fp16) times the packed 4-bit matrix [N, K], transposed."""
     (M, K), dtype, gpu = _rows("x", x)
-    shape, out, _ = _rows("y", y)
-    N = shape[1]
+    (rows, N), out, _ = _rows("y", y)
+    if rows != M:
+        _operand("y", y, (M, N), y.dtype, gpu)
     _check(lib().medusa_linear_i4(
-        dtype, _operand("x", x, x.shape, x.dtype, gpu), _packed_i4("packed", packed, N, K, group, zeros, gpu), M, N, K, group, int(zeros), out,
-        _operand("y", y, (M, N), y.dtype, gpu), None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu),
-        0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
+        dtype, _whole("x", x, gpu), _packed_i4("packed", packed, N, K, group, zeros, gpu), M, N, K, group, int(zeros), out, _whole("y", y, gpu),
+        None if ws is None else _whole("ws", ws, gpu), 0 if ws is None else ws.nbytes, _stream_of(gpu, stream)))
 
 
 def medusa_swiglu_i4(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, group: int, zeros: bool, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
                      stream=None) -> None:
     """y [M, ffn] = SiLU(x gate^T) * (x up^T): x [M, K] and y of bf16 or fp16, gate and up packed 4-bit matrices [ffn, K]."""
     (M, K), dtype, gpu = _rows("x", x)
-    shape, _, _ = _rows("y", y)
-    N = shape[1]
+    (rows, N), out, _ = _rows("y", y)
+    if rows != M or out != dtype:
+        _operand("y", y, (M, N), x.dtype, gpu)
     _check(lib().medusa_swiglu_i4(
-        dtype, _operand("x", x, x.shape, x.dtype, gpu), _packed_i4("gate", gate, N, K, group, zeros, gpu), _packed_i4("up", up, N, K, group, zeros, gpu),
-        M, N, K, group, int(zeros), _operand("y", y, (M, N), x.dtype, gpu), None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu),
-        0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
+        dtype, _whole("x", x, gpu), _packed_i4("gate", gate, N, K, group, zeros, gpu), _packed_i4("up", up, N, K, group, zeros, gpu), M, N, K, group, int(zeros),
+        _whole("y", y, gpu), None if ws is None else _whole("ws", ws, gpu), 0 if ws is None else ws.nbytes, _stream_of(gpu, stream)))
 
 
 # ---------------------------------------------------------------------------------------------
@@ -498,15 +505,17 @@ def medusa_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor, pr
     (rows, vocab), dtype, gpu = _rows("logits", logits)
     if rows_per_setting <= 0 or rows_per_setting >> 31:
         raise MedusaError(-1, f"sample: {rows_per_setting} rows per setting")
-    ld = logits.stride(0) if rows > 1 else vocab
-    if (vocab > 1 and logits.stride(1) != 1) or ld < vocab:
+    ld, step = logits.stride()
+    if rows <= 1:
+        ld = vocab
+    if (step != 1 and vocab > 1) or ld < vocab:
         raise MedusaError(-2, "logits: a row's logits must lie side by side, and rows must not overlap")
     n, f32 = (-(-rows // rows_per_setting),), torch.float32
     _check(lib().medusa_sample(
         dtype, logits.data_ptr(), ld, rows, vocab, _operand("temperature", temperature, n, f32, gpu), _operand("top_k", top_k, n, torch.int32, gpu),
         _operand("top_p", top_p, n, f32, gpu), _operand("min_p", min_p, n, f32, gpu), rows_per_setting, _operand("u", u, (rows,), f32, gpu),
         _operand("token", token, (rows,), torch.int32, gpu), _operand("prob", prob, (rows,), f32, gpu),
-        None if ws is None else _operand("ws", ws, ws.shape, ws.dtype, gpu), 0 if ws is None else ws.numel() * ws.element_size(), _stream_of(gpu, stream)))
+        None if ws is None else _whole("ws", ws, gpu), 0 if ws is None else ws.nbytes, _stream_of(gpu, stream)))
 
 
 def medusa_kv_bytes(kv: KvDesc) -> int:
