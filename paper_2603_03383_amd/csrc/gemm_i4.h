@@ -173,10 +173,10 @@ __device__ inline void multiply_tile(f32x4_t (&tot)[MT], const u32x4_t (&x)[4][M
   }
 }
 
-// Sums over WK waves that made the same outputs of their parts of the features, the activation, and the way out.  A workgroup's waves are WN groups of columns x
-// WK parts; `red`: LDS of WN x WK x MT x NT KiB.
-template <typename E, bool GATED, int MT, int NT, int WN, int WK>
-__device__ inline void finish_i4(const I4Product& p, const f32x4_t (&tot)[NT][MT], f32x4_t* red, int row0, int tile0, int wn, int wk, int lane) {
+// Sums over WK waves that made the same outputs of their parts of the features (wk: which of them), the activation, and the way out.  `red`: LDS of WK x MT x NT KiB,
+// not used where WK is 1.
+template <typename E, bool GATED, int MT, int NT, int WK>
+__device__ inline void finish_i4(const I4Product& p, const f32x4_t (&tot)[NT][MT], f32x4_t* red, int row0, int tile0, int wk, int lane) {
   constexpr int kTiles = MT * NT, kGateTiles = GATED ? NT / 2 : NT;
   auto put = [&](int i, int j, f32x4_t v, f32x4_t up) {
     if constexpr (GATED) {
@@ -198,14 +198,13 @@ __device__ inline void finish_i4(const I4Product& p, const f32x4_t (&tot)[NT][MT
       for (int j = 0; j < kGateTiles; ++j) put(i, j, tot[j][i], tot[GATED ? kGateTiles + j : j][i]);
   } else {
     __syncthreads();
-    f32x4_t* const mine = red + wn * WK * kTiles * 64;  // [part][tile][lane]
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) mine[(wk * kTiles + t) * 64 + lane] = tot[t % NT][t / NT];
+    for (int t = 0; t < kTiles; ++t) red[(wk * kTiles + t) * 64 + lane] = tot[t % NT][t / NT];  // [part][tile][lane]
     __syncthreads();
     auto sum = [&](int tile) {
-      f32x4_t v = mine[tile * 64 + lane];
+      f32x4_t v = red[tile * 64 + lane];
 #pragma unroll
-      for (int w = 1; w < WK; ++w) v += mine[(w * kTiles + tile) * 64 + lane];
+      for (int w = 1; w < WK; ++w) v += red[(w * kTiles + tile) * 64 + lane];
       return v;
     };
     for (int t = wk; t < MT * kGateTiles; t += WK) {
@@ -343,26 +342,25 @@ __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
   }
 done:
 
-  finish_i4<E, GATED, MT, NT, 1, NW>(p, tot, reinterpret_cast<f32x4_t*>(lds_raw), row0, tile0, 0, wave, lane);
+  finish_i4<E, GATED, MT, NT, NW>(p, tot, reinterpret_cast<f32x4_t*>(lds_raw), row0, tile0, wave, lane);
 }
 
-// More rows.  A workgroup makes 16 WM MT rows x WN NT tiles of columns with WM x WN waves, WK times over: each of the WK parts has its own blocks of
-// features, and their sums meet in LDS at the end.  X, codes, scales and zero points go straight to an LDS ring (`global_load_lds`, 16 bytes
-// per lane, no registers) in turns of WK blocks; one counted wait and one barrier per turn make a turn everyone's, and behind it the place of the turn
-// that all have read is requested anew.
+// More rows.  A workgroup makes 16 MT rows x NW NT tiles of columns with NW waves, which share the rows.  X, codes, scales and zero points go straight to an
+// LDS ring of two turns (`global_load_lds`, 16 bytes per lane, no registers), a turn for each block of features; one wait and one barrier make a turn
+// everyone's, and behind it the place of the turn that all have read is requested anew.  Two turns, so that a CU has two workgroups or three: their phases of
+// loads, LDS reads, conversions and products then overlap.  (One workgroup of eight waves and three turns, all in step: gated 1024 x 11008 x 4096 219 us
+// where two of four waves take 200, 64 x 128000 x 4096 85 and 81.)
 // Bound by the matrix cores and the vector units, which convert codes and scale sums: gated 1024 x 11008 x 4096 in 194-204 us (0.90-0.95 PFLOP/s; each is busy for half of the
 // clocks, and they overlap little), gated 200 x 12800 x 4096 in groups of 64 with zero points 88, 64 x 128000 x 4096 87 (3.6 TB/s).  64 rows to a wave, so that a
 // converted tile serves four products; 256 columns to four waves, or 128 where that fills the CUs better (kI4Cuts).
-template <int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int NS>
+template <int G, bool ZEROS, bool GATED, int MT, int NT, int NW>
 struct I4Ring {
-  static constexpr int kWaves = WM * WN * WK, kRows = WM * MT * 16, kMats = GATED ? 2 : 1, kTiles = WN * NT / kMats;  // tiles of each matrix
+  static constexpr int kRows = MT * 16, kMats = GATED ? 2 : 1, kTiles = NW * NT / kMats;  // tiles of each matrix
   // 1 KiB pieces of a block: X (four rows), codes (a tile), scales, zero points
   static constexpr int kX = kRows / 4, kScales = (kTiles * 32 * G + 1023) / 1024, kZeros = ZEROS ? (kTiles * 16 * G + 1023) / 1024 : 0;
   static constexpr int kAtScales = kX + kMats * kTiles, kAtZeros = kAtScales + kMats * kScales, kPieces = kAtZeros + kMats * kZeros;
-  static constexpr int kLoads = (WK * kPieces + kWaves - 1) / kWaves;  // per turn and wave
-  static constexpr int kTurn = WK * kPieces * 1024, kSum = WK > 1 ? kWaves * MT * NT * 1024 : 0;
-  static constexpr int kLds = NS * kTurn > kSum ? NS * kTurn : kSum;
-  static_assert(NS >= 2, "a turn is requested before it is read");
+  static constexpr int kLoads = (kPieces + NW - 1) / NW;  // per turn and wave
+  static constexpr int kTurn = kPieces * 1024, kLds = 2 * kTurn;
 };
 // a pointer that is the same in every lane, in scalar registers
 __device__ inline const uint8_t* uniform(const uint8_t* p) {
@@ -371,29 +369,20 @@ __device__ inline const uint8_t* uniform(const uint8_t* p) {
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)), lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
   return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
 }
-// all but the youngest `n` turns of L loads each have landed, for n <= NS
-template <int L, int NS>
-__device__ inline void wait_turns(int n) {
-  if (n >= NS) wait_loads<NS * L>();
-  else static_for<NS>([&](auto i) {
-    if (n == decltype(i)::value) wait_loads<decltype(i)::value * L>();
-  });
-}
-
-template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int NS, int WPE>
-__global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4Product p) {
-  typedef I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, NS> R;
-  constexpr int NW = R::kWaves, L = R::kLoads;
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int NW, int WPE>
+__global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_rows_kernel(I4Product p) {
+  typedef I4Ring<G, ZEROS, GATED, MT, NT, NW> R;
+  constexpr int L = R::kLoads;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds_raw[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q4 = lane >> 4, r16 = lane & 15, wk = wave / (WM * WN), wm = wave % WM, wn = wave / WM % WN;
+  const int q4 = lane >> 4, r16 = lane & 15;
   // Workgroups go round-robin to the 8 XCDs: each takes an eighth of the blocks, a column block's row blocks one after the other, which then
   // share its weights through the XCD's L2.
   const int xcd = blockIdx.x & 7, blocks = p.nb_m * p.nb_n;
   const int block = (int)((int64_t)blocks * xcd >> 3) + (int)(blockIdx.x >> 3);
   if (block >= (int)((int64_t)blocks * (xcd + 1) >> 3)) return;
   const int row0 = block % p.nb_m * R::kRows, tile0 = block / p.nb_m * R::kTiles;
-  const int last_row = p.M - 1 - row0, last_tile = p.n_tiles - 1 - tile0, turns = (p.n_blocks + WK - 1) / WK;
+  const int last_row = p.M - 1 - row0, last_tile = p.n_tiles - 1 - tile0;
   const uint32_t lds0 = MDZ_LDS_ADDR(lds_raw);
 
   // A wave's loads of a turn: where the piece's memory begins, a lane's place in it, how far the next block is.  (Loads beyond the last piece repeat it;
@@ -401,17 +390,17 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4
   // chunk of its row that stands in its place: chunk c of row r is at c ^ (r % 16), so that 16 rows' chunks are read without bank conflicts.
   const uint8_t* base[L];
   uint32_t off[L], chunk[L];
-  int step[L], dst[L], part[L];
+  int step[L], dst[L];
   static_for<L>([&](auto i) {
     constexpr int q = decltype(i)::value;
-    const int u = min(q * NW + wave, WK * R::kPieces - 1), v = u % R::kPieces;
-    dst[q] = u * 1024, part[q] = u / R::kPieces;
+    const int v = min(q * NW + wave, R::kPieces - 1);
+    dst[q] = v * 1024;
     if (v < R::kX) {
       const int row = v * 4 + q4;
       base[q] = reinterpret_cast<const uint8_t*>(p.X) + (int64_t)row0 * p.ldx, step[q] = 2 * kI4Block;
       off[q] = (uint32_t)min(row, last_row) * (uint32_t)p.ldx, chunk[q] = (r16 ^ (row & 15)) * 16;
     } else {
-      const int kind = v < R::kAtScales ? 0 : v < R::kAtZeros ? 1 : 2, size = kind == 0 ? 1024 : kind == 1 ? 32 * G : 16 * G;
+      const int kind = v < R::kAtScales ? 0 : !ZEROS || v < R::kAtZeros ? 1 : 2, size = kind == 0 ? 1024 : kind == 1 ? 32 * G : 16 * G;
       const int c = v - (kind == 0 ? R::kX : kind == 1 ? R::kAtScales : R::kAtZeros), per = kind == 0 ? R::kTiles : kind == 1 ? R::kScales : max(R::kZeros, 1);
       const I4Matrix w = GATED && c >= per ? p.w[1] : p.w[0];
       const int at = c % per * 1024 + lane * 16, tile = min(min(at / size, R::kTiles - 1), last_tile);
@@ -419,13 +408,12 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4
       off[q] = (uint32_t)tile * (uint32_t)p.n_blocks * (uint32_t)size + at % size, chunk[q] = 0;
     }
     base[q] = uniform(base[q]), step[q] = __builtin_amdgcn_readfirstlane(step[q]);
-    dst[q] = __builtin_amdgcn_readfirstlane(dst[q]), part[q] = __builtin_amdgcn_readfirstlane(part[q]);
+    dst[q] = __builtin_amdgcn_readfirstlane(dst[q]);
   });
-  auto request = [&](int t) {
-    const uint32_t slot = lds0 + t % NS * R::kTurn;
+  auto request = [&](int b) {
+    const uint32_t slot = lds0 + b % 2 * R::kTurn;
     static_for<L>([&](auto i) {
       constexpr int q = decltype(i)::value;
-      const int b = min(t * WK + part[q], p.n_blocks - 1);
       // (the last chunk again for those beyond K, whose codes are their zero points)
       const uint32_t o = off[q] + min(chunk[q], (uint32_t)(p.K - 8 - b * kI4Block) * 2);
       load_to_lds<0>(base[q] + (uint32_t)(b * step[q]), o, slot + dst[q]);
@@ -439,28 +427,25 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4
     for (int i = 0; i < MT; ++i) tot[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const I4Constants<E> constants;
 
-  static_for<NS - 1>([&](auto i) {
-    if (decltype(i)::value < turns) request(decltype(i)::value);
-  });
-  for (int t = 0; t < turns; ++t) {
+  request(0);
+  for (int b = 0; b < p.n_blocks; ++b) {
     wait_lds();
-    wait_turns<L, NS - 2>(turns - 1 - t);
+    wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + NS - 1 < turns) request(t + NS - 1);
-    if (WK > 1 && t * WK + wk >= p.n_blocks) continue;
-    const uint8_t* const xs = lds_raw + t % NS * R::kTurn + wk * (R::kPieces * 1024);
+    if (b + 1 < p.n_blocks) request(b + 1);
+    const uint8_t* const xs = lds_raw + b % 2 * R::kTurn;
     u32x4_t x[4][MT];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int i = 0; i < MT; ++i)
-        x[s][i] = *reinterpret_cast<const u32x4_t*>(xs + ((wm * MT + i) * 16 + r16) * 256 + (((s * 4 + q4) ^ r16) * 16));
+        x[s][i] = *reinterpret_cast<const u32x4_t*>(xs + (i * 16 + r16) * 256 + (((s * 4 + q4) ^ r16) * 16));
     f32x4_t c0[G][MT];
     sum_block<E, G, ZEROS>(c0, x);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int mat = GATED && j >= NT / 2, tile = wn * (NT / R::kMats) + (GATED ? j % (NT / 2) : j);
+      const int mat = GATED && j >= NT / 2, tile = wave * (NT / R::kMats) + (GATED ? j % (NT / 2) : j);
       const uint8_t* const cs = xs + (R::kX + mat * R::kTiles + tile) * 1024 + lane * 16;
       const uint8_t* const ss = xs + (R::kAtScales + mat * R::kScales) * 1024 + tile * (32 * G) + q4 * (8 * G);
       I4Zeros<E, G> z{};
@@ -472,7 +457,7 @@ __global__ void __launch_bounds__(WM * WN * WK * 64, WPE) gemm_i4_rows_kernel(I4
 #pragma unroll
       for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(tot[j][i]));
   }
-  finish_i4<E, GATED, MT, NT, WM * WN, WK>(p, tot, reinterpret_cast<f32x4_t*>(lds_raw), row0 + wm * MT * 16, tile0 + wn * (NT / R::kMats), wn * WM + wm, wk, lane);
+  finish_i4<E, GATED, MT, NT, 1>(p, tot, nullptr, row0, tile0 + wave * (NT / R::kMats), 0, lane);
 }
 
 template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D, int DX, int WPE>
@@ -488,25 +473,22 @@ static int launch_i4_few(I4Product p, hipStream_t st) {
   return MDZ_OK;
 }
 
-template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int WM, int WN, int WK, int WPE>
+template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int NW, int WPE>
 static int launch_i4_rows(I4Product p, hipStream_t st) {
-  // Two turns, so that a CU has two workgroups or three: their phases of loads, LDS reads, conversions and products then overlap.  (One workgroup of eight waves and
-  // three turns, all in step: gated 1024 x 11008 x 4096 219 us where two of four waves take 200, 64 x 128000 x 4096 85 and 81.)
-  constexpr int NS = 2;
-  typedef I4Ring<G, ZEROS, GATED, MT, NT, WM, WN, WK, NS> R;
+  typedef I4Ring<G, ZEROS, GATED, MT, NT, NW> R;
   static_assert(R::kLds <= 80 * 1024, "two workgroups share a CU's LDS");
   p.nb_m = (p.M + R::kRows - 1) / R::kRows, p.nb_n = (p.n_tiles + R::kTiles - 1) / R::kTiles;
   const int64_t workgroups = ((int64_t)p.nb_m * p.nb_n + 7) / 8 * 8;
-  MDZ_REQUIRE(workgroups * R::kWaves * 64 <= (int64_t)UINT32_MAX, MDZ_EUNSUPPORTED, "linear_i4: %d x %d outputs are more than one launch takes", p.M, p.N);
-  auto kernel = gemm_i4_rows_kernel<E, G, ZEROS, GATED, MT, NT, WM, WN, WK, NS, WPE>;
+  MDZ_REQUIRE(workgroups * NW * 64 <= (int64_t)UINT32_MAX, MDZ_EUNSUPPORTED, "linear_i4: %d x %d outputs are more than one launch takes", p.M, p.N);
+  auto kernel = gemm_i4_rows_kernel<E, G, ZEROS, GATED, MT, NT, NW, WPE>;
   MDZ_SET_LDS_ONCE(kernel, R::kLds);
-  launch_timed(PROF_GEMM_I4, kernel, dim3((unsigned)workgroups), R::kWaves * 64, R::kLds, st, p);
+  launch_timed(PROF_GEMM_I4, kernel, dim3((unsigned)workgroups), NW * 64, R::kLds, st, p);
   MDZ_LAUNCH_CHECK();
   return MDZ_OK;
 }
 
 // few rows: rows / 16, tiles, pieces of X, waves; blocks of weights and of X requested ahead, waves per SIMD that the registers allow
-// more rows: rows / 16 and tiles of a wave, waves of rows, of columns and of features, waves per SIMD
+// more rows: rows / 16 and tiles of a wave, waves, waves per SIMD
 #define MDZ_I4_CASES                    \
   MDZ_I4_FEW(1, 1, 1, 8, 8, 8, 2)       \
   MDZ_I4_FEW(1, 2, 1, 8, 4, 4, 2)       \
@@ -526,17 +508,17 @@ static int launch_i4_rows(I4Product p, hipStream_t st) {
   MDZ_I4_FEW(4, 1, 16, 8, 4, 1, 2)      \
   MDZ_I4_FEW(4, 2, 16, 8, 2, 1, 2)      \
   MDZ_I4_FEW(4, 6, 16, 4, 2, 1, 1)      \
-  MDZ_I4_ROWS(4, 2, 1, 4, 1, 2)         \
-  MDZ_I4_ROWS(4, 4, 1, 4, 1, 2)
+  MDZ_I4_ROWS(4, 2, 4, 2)               \
+  MDZ_I4_ROWS(4, 4, 4, 2)
 template <typename E, int G, bool ZEROS, bool GATED>
 static int launch_i4_tiles(const I4Product& p, const I4Plan& plan, hipStream_t st) {
   constexpr int kKind = i4_kind(__is_same(E, f16_t), G, ZEROS);
 #define MDZ_I4_FEW(MT, NT, XR, NW, D, DX, WPE)                                                        \
-  if constexpr ((!GATED || NT % 2 == 0) && i4_built(I4Plan{MT, NT, 0, 0, NW, XR}, kKind, GATED))       \
-    if (plan.wm == 0 && plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.wk == NW)              \
+  if constexpr ((!GATED || NT % 2 == 0) && i4_built(I4Plan{MT, NT, NW, XR}, kKind, GATED))             \
+    if (plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.waves == NW)                           \
       return launch_i4_few<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>(p, st);
-#define MDZ_I4_ROWS(MT, NT, WM, WN, WK, WPE) \
-  if (plan.mt == MT && plan.nt == NT && plan.wm == WM && plan.wn == WN && plan.wk == WK) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, WM, WN, WK, WPE>(p, st);
+#define MDZ_I4_ROWS(MT, NT, NW, WPE) \
+  if (plan.mt == MT && plan.nt == NT && plan.xr == 0 && plan.waves == NW) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, NW, WPE>(p, st);
   MDZ_I4_CASES
   MDZ_FAIL(MDZ_EINVAL, "linear_i4: no kernel of %d x %d tiles", plan.mt, plan.nt);
 }

@@ -119,16 +119,16 @@ static I4Plan plan_i4(int M, int N, int K, int kind, bool gated) {
   if (M <= 16) {
     const int xr = M <= 4 ? 1 : M <= 8 ? 2 : 4;
     const bool of_32 = kind == 2 || kind == 5 || kind == 7;
-    const I4Plan two{1, 2, 0, 0, kind == 5 ? 8 : 4, xr}, four{1, 4, 0, 0, 4, xr};
-    if (gated) return tiles <= cus ? I4Plan{1, 2, 0, 0, 8, xr} : of_32 || (tiles <= 4 * cus && xr < 4) ? two : four;
-    return tiles <= cus ? I4Plan{1, 1, 0, 0, 8, xr} : of_32 || tiles <= 2 * cus ? two : four;
+    const I4Plan two{1, 2, kind == 5 ? 8 : 4, xr}, four{1, 4, 4, xr};
+    if (gated) return tiles <= cus ? I4Plan{1, 2, 8, xr} : of_32 || (tiles <= 4 * cus && xr < 4) ? two : four;
+    return tiles <= cus ? I4Plan{1, 1, 8, xr} : of_32 || tiles <= 2 * cus ? two : four;
   }
   I4Plan best{};
   float least = INFINITY;
   for (const I4Cut& c : kI4Cuts) {
     const int wide = gated ? c.gate_tiles : c.tiles;
     if (M < c.least_rows || M > c.most_rows || wide == 0 || c.us[kind] == 0.f) continue;
-    if (c.plan.wm == 0 && (M + c.rows - 1) / c.rows > kMaxGridY) continue;  // (its rows are the grid's second axis)
+    if (c.plan.xr != 0 && (M + c.rows - 1) / c.rows > kMaxGridY) continue;  // (its rows are the grid's second axis)
     const int64_t wgs = ((int64_t)(M + c.rows - 1) / c.rows) * ((tiles + wide - 1) / wide), at_once = c.us_two[kind] > 0.f ? 2 * cus : cus;
     const int64_t full = wgs / at_once, rest = wgs % at_once;
     const float us_full = at_once > cus ? c.us_two[kind] : c.us[kind], us_rest = rest > cus ? us_full : rest > 0 ? c.us[kind] : 0.f;
@@ -183,7 +183,7 @@ static int product_i4(const char* what, int dtype, const void* x, const void* pa
   hipStream_t st = (hipStream_t)stream;
   const bool z = zeros != 0, gated = second != nullptr;
   p.ldx = (int64_t)K * 2;
-  if (plan.wm > 0 && (K % 8 != 0 || reinterpret_cast<uintptr_t>(x) % 16 != 0)) {  // loads to LDS take 16 bytes from addresses of 16
+  if (plan.xr == 0 && (K % 8 != 0 || reinterpret_cast<uintptr_t>(x) % 16 != 0)) {  // loads to LDS take 16 bytes from addresses of 16
     const int64_t chunks = need / 16;
     MDZ_REQUIRE(chunks <= (int64_t)UINT32_MAX - 255, MDZ_EUNSUPPORTED, "%s: %d unaligned rows are more than one launch takes", what, M);
     launch_timed(PROF_GEMM_I4, align_rows_i4_kernel, (unsigned)((chunks + 255) / 256), 256, 0, st, (const uint16_t*)x, K, (u32x4_t*)ws, chunks,

@@ -52,10 +52,10 @@ struct I4Product {
   int nb_m, nb_n;  // workgroups of rows and of columns
 };
 
-// How a product is cut: rows / 16 and tiles (a gated product's are half gate, half up) of a wave, waves of rows (0: the kernel of few rows), of columns and of
-// features, and for few rows the pieces of four of them that are loaded.
+// How a product is cut: rows / 16 and tiles (a gated product's are half gate, half up) of a wave, waves of a workgroup, and for few rows the pieces of four of them that
+// are loaded (0: the kernel of more rows).
 struct I4Plan {
-  int mt, nt, wm, wn, wk, xr;
+  int mt, nt, waves, xr;
 };
 // Whether q - z is made before the products (gemm_i4.h), and what a product costs by: 0 .. 2 groups of 128, 64 and 32 without zero points, 3 .. 5 with them,
 // 6 and 7 groups of 64 and 32 whose zero points are subtracted.
@@ -73,21 +73,21 @@ struct I4Cut {
   float us[8], us_two[8];
 };
 constexpr I4Cut kI4Cuts[] = {
-    {{2, 1, 0, 0, 8, 8}, 17, 32, 32, 1, 0, 8, {1.48f, 1.52f, 1.69f, 1.6f, 1.64f, 1.9f, 1.58f, 1.72f}, {}},
-    {{2, 2, 0, 0, 8, 8}, 17, 32, 32, 2, 1, 8, {2.0f, 2.1f, 2.33f, 2.25f, 2.35f, 2.77f, 2.28f, 2.56f}, {}},
-    {{2, 6, 0, 0, 4, 8}, 17, 32, 32, 6, 3, 4, {2.05f, 2.35f, 3.2f, 2.35f, 3.4f, 4.15f, 3.2f, 3.9f}, {}},
-    {{4, 1, 0, 0, 8, 16}, 33, 1 << 30, 64, 1, 0, 8, {2.55f, 2.6f, 4.0f, 2.7f, 2.95f, 4.05f, 2.62f, 2.75f}, {}},
-    {{4, 2, 0, 0, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, {3.05f, 0.f, 0.f, 3.3f, 0.f, 0.f, 3.17f, 0.f}, {}},
-    {{4, 6, 0, 0, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, {3.05f, 3.7f, 0.f, 3.7f, 0.f, 0.f, 4.0f, 0.f}, {}},
-    {{4, 2, 1, 4, 1, 0}, 17, 1 << 30, 64, 8, 4, 1, {0.95f, 1.0f, 1.16f, 1.15f, 1.22f, 1.54f, 1.04f, 1.2f}, {1.2f, 1.25f, 1.53f, 1.36f, 1.55f, 2.0f, 1.46f, 1.67f}},
-    {{4, 4, 1, 4, 1, 0}, 17, 1 << 30, 64, 16, 8, 1, {1.38f, 1.43f, 2.05f, 1.55f, 1.85f, 2.43f, 1.69f, 2.07f}, {2.12f, 2.35f, 2.87f, 2.33f, 4.1f, 3.42f, 2.65f, 3.1f}},
+    {{2, 1, 8, 8}, 17, 32, 32, 1, 0, 8, {1.48f, 1.52f, 1.69f, 1.6f, 1.64f, 1.9f, 1.58f, 1.72f}, {}},
+    {{2, 2, 8, 8}, 17, 32, 32, 2, 1, 8, {2.0f, 2.1f, 2.33f, 2.25f, 2.35f, 2.77f, 2.28f, 2.56f}, {}},
+    {{2, 6, 4, 8}, 17, 32, 32, 6, 3, 4, {2.05f, 2.35f, 3.2f, 2.35f, 3.4f, 4.15f, 3.2f, 3.9f}, {}},
+    {{4, 1, 8, 16}, 33, 1 << 30, 64, 1, 0, 8, {2.55f, 2.6f, 4.0f, 2.7f, 2.95f, 4.05f, 2.62f, 2.75f}, {}},
+    {{4, 2, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, {3.05f, 0.f, 0.f, 3.3f, 0.f, 0.f, 3.17f, 0.f}, {}},
+    {{4, 6, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, {3.05f, 3.7f, 0.f, 3.7f, 0.f, 0.f, 4.0f, 0.f}, {}},
+    {{4, 2, 4, 0}, 17, 1 << 30, 64, 8, 4, 1, {0.95f, 1.0f, 1.16f, 1.15f, 1.22f, 1.54f, 1.04f, 1.2f}, {1.2f, 1.25f, 1.53f, 1.36f, 1.55f, 2.0f, 1.46f, 1.67f}},
+    {{4, 4, 4, 0}, 17, 1 << 30, 64, 16, 8, 1, {1.38f, 1.43f, 2.05f, 1.55f, 1.85f, 2.43f, 1.69f, 2.07f}, {2.12f, 2.35f, 2.87f, 2.33f, 4.1f, 3.42f, 2.65f, 3.1f}},
 };
 // Whether the kernel of few rows has this cut for this kind.  Up to 16 rows groups of 32 take two tiles at most, with eight waves where zero points cost registers.
 constexpr bool i4_built(const I4Plan& plan, int kind, bool gated) {
   const bool of_32 = kind == 2 || kind == 5 || kind == 7;
-  if (plan.mt == 1) return !(of_32 && plan.nt == 4) && !(kind == 5 && plan.nt == 2 && plan.wk == 4) && (gated || kind == 5 || !(plan.nt == 2 && plan.wk == 8));
+  if (plan.mt == 1) return !(of_32 && plan.nt == 4) && !(kind == 5 && plan.nt == 2 && plan.waves == 4) && (gated || kind == 5 || !(plan.nt == 2 && plan.waves == 8));
   for (const I4Cut& c : kI4Cuts)
-    if (c.plan.wm == 0 && c.plan.mt == plan.mt && c.plan.nt == plan.nt) return c.us[kind] > 0.f;
+    if (c.plan.xr != 0 && c.plan.mt == plan.mt && c.plan.nt == plan.nt) return c.us[kind] > 0.f;
   return false;
 }
 
