@@ -414,10 +414,26 @@ __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_rows_kernel(I4Product p)
     const uint32_t slot = lds0 + b % 2 * R::kTurn;
     static_for<L>([&](auto i) {
       constexpr int q = decltype(i)::value;
-      // (the last chunk again for those beyond K, whose codes are their zero points)
+      // (the last chunk again for those beyond K: a load stays inside its row; clear_behind_k)
       const uint32_t o = off[q] + min(chunk[q], (uint32_t)(p.K - 8 - b * kI4Block) * 2);
       load_to_lds<0>(base[q] + (uint32_t)(b * step[q]), o, slot + dst[q]);
     });
+  };
+  // Zeros in place of the chunks beyond K, in the pieces of X that this wave has loaded.  (The codes there are their zero points, but products with 16 + q and
+  // what is taken off them cancel in exact arithmetic alone: with the last chunk up to sixteen times in the sums these lost four bits, and overflowed where all
+  // that they stand for is far inside fp32's range.)
+  auto clear_behind_k = [&](int b) {
+    static_assert(R::kX % NW == 0, "a wave's first loads are its pieces of X");
+    // (the lane's number made anew, from a zero that the compiler does not know: no register is held through the loop for it)
+    uint32_t l = 0;
+    asm volatile("" : "+v"(l));
+    l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, l));
+#pragma unroll
+    for (int q = 0; q < R::kX / NW; ++q) {
+      const uint32_t v = q * NW + wave, row = v * 4 + (l >> 4), at = (l & 15) ^ (row & 15);
+      if ((int)at * 8 >= p.K - b * kI4Block) *reinterpret_cast<u32x4_t*>(lds_raw + b % 2 * R::kTurn + v * 1024 + l * 16) = u32x4_t{0, 0, 0, 0};
+    }
+    wait_lds();
   };
 
   f32x4_t tot[NT][MT];
@@ -431,6 +447,7 @@ __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_rows_kernel(I4Product p)
   for (int b = 0; b < p.n_blocks; ++b) {
     wait_lds();
     wait_loads<0>();
+    if ((b + 1) * kI4Block > p.K) clear_behind_k(b);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (b + 1 < p.n_blocks) request(b + 1);
