@@ -299,7 +299,8 @@ int medusa_swiglu_i4(int dtype, const void* x, const void* gate_packed, const vo
  * sampling token by token gives with these random numbers, and next_root the token drawn after it.
  * Outputs must not overlap inputs or each other.
  * ws: medusa_sample_workspace_bytes(rows, vocab) bytes of scratch that start on 16 bytes (0: ws may be NULL); nothing in it has
- * to be set, and nothing is kept in it. */
+ * to be set, and nothing is kept in it.  They serve calls of fewer rows and of smaller vocabularies too (rows as many as the GPU has
+ * CUs, or more, use none of it themselves: a call of so many alone takes NULL and 0). */
 int64_t medusa_sample_workspace_bytes(int rows, int vocab);
 int medusa_sample(int dtype, const void* logits, int64_t ld, int rows, int vocab, const float* temperature_opt,
                   const int32_t* top_k_opt, const float* top_p_opt, const float* min_p_opt, int rows_per_setting,

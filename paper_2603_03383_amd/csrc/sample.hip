@@ -951,6 +951,7 @@ __global__ void __launch_bounds__(kRowThreads) sample_row_kernel(SampleArgs a) {
 // ---- the call ----------------------------------------------------------------------------------------------
 constexpr int kMaxVocab = 1 << 24;  // the masses then still have 38 bits behind the point
 static bool sample_splits(int rows, int vocab) { return vocab > 2 * kChunk && rows < num_cus(); }
+// scratch of a call
 static int64_t sample_bytes(int rows, int vocab) {
   if (!sample_splits(rows, vocab)) return 0;
   const int64_t chunks = (vocab + kChunk - 1) / kChunk;
@@ -997,7 +998,8 @@ extern "C" {
 
 int64_t medusa_sample_workspace_bytes(int rows, int vocab) {
   const int rc = check_sample(rows, vocab);
-  return rc ? rc : sample_bytes(rows, vocab);
+  // (of the call of up to so many rows that needs most: one of many more, whose rows are not split, needs none itself)
+  return rc ? rc : sample_bytes(rows < num_cus() ? rows : num_cus() - 1, vocab);
 }
 
 int medusa_sample(int dtype, const void* logits, int64_t ld, int rows, int vocab, const float* temperature_opt, const int32_t* top_k_opt,
