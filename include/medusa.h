@@ -262,7 +262,7 @@ int medusa_pack_weight_i4(int dtype, const void* src, int64_t n_rows, int64_t k,
 
 /* The same for a matrix that is in 4 bits already: codes [n_rows, k], one per byte, scales [n_rows, ceil(k / group)] of type
  * dtype, zeros_opt (nullable: a matrix without zero points) [n_rows, ceil(k / group)].  Of codes and zero points the lower
- * four bits count. */
+ * four bits count: a zero point of 16, which layouts that store z - 1 can express, has no place here and would be taken as 0. */
 int medusa_pack_codes_i4(int dtype, const uint8_t* codes, const void* scales, const uint8_t* zeros_opt, int64_t n_rows,
                          int64_t k, int group, void* dst, int64_t dst_rows, int64_t tile_offset, void* stream);
 
@@ -293,10 +293,12 @@ int medusa_swiglu_i4(int dtype, const void* x, const void* gate_packed, const vo
  * not above zero stands for the row's first token.  NaN and minus infinity cannot be drawn; beside plus infinity nothing else
  * can; a row in which nothing can be drawn gets token -1 and prob 0.  u outside [0, 1) is taken as its nearer end.
  * Settings lie in device memory, one for every rows_per_setting rows in a row (a tree's nodes): [ceil(rows / rows_per_setting)] each;
- * NULL: temperature 1, no top-k, no top-p, no min-p.  Masses are 64-bit integers in steps of at most 2^-(61 - b) of the largest, b the bits of
- * vocab (at most 2^24), and their sums are exact: a row's token depends on nothing but the row.
+ * NULL: temperature 1, no top-k, no top-p, no min-p.  Masses are 64-bit integers in steps of 2^-S of the largest, S = 62 -
+ * ceil(log2(vocab)) but at most 50 (vocab at most 2^24); an exponential is within 2^-45 of itself before it is rounded to
+ * that.  Their sums are exact: a row's token depends on nothing but the row.
  * Drawn at every node of a tree, the tokens take node_argmax's place in accept_longest_prefix: the path is then one that
- * sampling token by token gives with these random numbers, and next_root the token drawn after it.
+ * sampling token by token gives with these random numbers, and next_root the token drawn after it.  (A token of -1 matches no
+ * node.  As next_root it ends the text: a step that is given it all the same reads the embedding of token 0.)
  * Outputs must not overlap inputs or each other.
  * ws: medusa_sample_workspace_bytes(rows, vocab) bytes of scratch that start on 16 bytes (0: ws may be NULL); nothing in it has
  * to be set, and nothing is kept in it.  They serve calls of fewer rows and of smaller vocabularies too (rows as many as the GPU has
