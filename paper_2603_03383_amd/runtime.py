@@ -254,14 +254,17 @@ def run_step(model: DeviceModel, kv: DeviceKV, buf: StepBuffers, hidden, src_row
     """Enqueues heads -> verify -> accept -> compact (the four C-ABI calls, nothing else).  With `sampling` the tokens that the
     model gives at the nodes are drawn from its logits (buf needs them: want_logits) and take the place of the likeliest."""
     Bn = buf.batch
+    if sampling is not None:  # (before anything is enqueued)
+        if buf.logits is None:
+            raise B.MedusaError(-1, "sampling: the step's buffers hold no logits (want_logits)")
+        if sampling.u.shape != buf.node_argmax.shape:
+            raise B.MedusaError(-2, f"sampling: for {tuple(sampling.u.shape)} nodes, the step has {tuple(buf.node_argmax.shape)}")
     if with_heads:
         B.medusa_heads(model.desc, model.weights, hidden, src_row, root_token, Bn, hidden.shape[1], buf.cand_flat,
                        buf.tree_tokens, buf.head_logits, buf.ws, stream)
     B.tree_verify_step(model.desc, model.weights, buf.tree_tokens, kv.desc, seq_len, Bn, buf.max_prefix,
                        buf.node_argmax, buf.hidden, buf.logits, buf.ws, stream)
     if sampling is not None:
-        if buf.logits is None:
-            raise B.MedusaError(-1, "sampling: the step's buffers hold no logits (want_logits)")
         sampling.draw(buf.logits, buf.node_argmax, stream)
     B.accept_longest_prefix(model.tree, buf.tree_tokens, buf.node_argmax, Bn, buf.accept_len, buf.best_path,
                             buf.acc_nodes, buf.acc_tokens, buf.next_root, buf.last_node, stream)
