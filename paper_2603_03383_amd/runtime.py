@@ -246,6 +246,8 @@ class Sampling:
 
     def draw(self, logits: torch.Tensor, tokens: torch.Tensor, stream=None) -> None:
         """logits [batch, T, vocab] -> tokens [batch, T] (and their probabilities, in `prob`)."""
+        if not tokens.is_contiguous():  # (flattened they would be a copy)
+            raise B.MedusaError(-2, "tokens: tensors handed to the library must be contiguous")
         B.medusa_sample(logits.flatten(0, 1), self.u.flatten(), tokens.flatten(), self.prob.flatten(), ws=self.ws, stream=stream, **self.settings)
 
 

@@ -1,4 +1,4 @@
-"""Sampling put into a step: what cannot be drawn is refused before anything of the step is enqueued."""
+"""Sampling put into a step: what cannot be drawn is refused before anything of the step is enqueued, and drawn tokens reach the buffer that was given."""
 import types
 
 import pytest
@@ -62,4 +62,12 @@ def test_a_step_without_logits_is_refused_whole(calls):
 def test_sampling_of_another_batch_is_refused_whole(calls, batch):
     with pytest.raises(P.MedusaError) as e:
         _step(_buffers(), runtime.Sampling(_model(), batch))
+    assert e.value.status == ESHAPE and calls == []
+
+
+def test_tokens_that_do_not_lie_side_by_side_are_refused(calls):
+    """A flattened copy of them would be drawn into, and lost."""
+    sampling = runtime.Sampling(_model(), BATCH)
+    with pytest.raises(P.MedusaError) as e:
+        sampling.draw(torch.zeros(BATCH, T, VOCAB), torch.zeros(BATCH, T + 1, dtype=torch.int32)[:, :T])
     assert e.value.status == ESHAPE and calls == []
