@@ -293,6 +293,12 @@ def _int32(what: str, *sizes: int) -> None:
         raise MedusaError(-3, f"{what}: {sizes}: sizes up to 2^31 - 1")
 
 
+def _fits(what: str, bits: int, *numbers: int) -> None:
+    """The same for numbers that may lie below zero too."""
+    if any(n >> (bits - 1) not in (0, -1) for n in numbers):
+        raise MedusaError(-3, f"{what}: {numbers}: {bits}-bit integers")
+
+
 def _rows(name: str, t: torch.Tensor):
     """(shape, storage dtype, GPU) of a tensor of rows."""
     shape, dtype = t.shape, _STORAGE.get(t.dtype)
@@ -420,6 +426,8 @@ MDZ_I4_TILE_ROWS = 16
 
 @functools.lru_cache(maxsize=None)
 def medusa_packed_i4_bytes(n_rows: int, k: int, group: int, zeros: bool = False) -> int:
+    _fits("packed_i4_bytes", 64, n_rows, k)
+    _fits("packed_i4_bytes", 32, group, int(zeros))
     return _check(lib().medusa_packed_i4_bytes(n_rows, k, group, int(zeros)))
 
 
@@ -432,7 +440,7 @@ def _whole(name: str, t: torch.Tensor, device: int) -> int:
 
 def _packed_i4(name: str, t: torch.Tensor, n: int, k: int, group: int, zeros: bool, device: int) -> int:
     """Scales and zero points stand where the codes end: a buffer of other sizes was packed for another matrix."""
-    got, want = t.nbytes, medusa_packed_i4_bytes(n, k, group, bool(zeros))
+    got, want = t.nbytes, medusa_packed_i4_bytes(n, k, group, zeros)
     if got != want:
         raise MedusaError(-2, f"{name}: {got} bytes are not those of [{n}, {k}] in groups of {group}, {want}")
     return _whole(name, t, device)
@@ -441,6 +449,7 @@ def _packed_i4(name: str, t: torch.Tensor, n: int, k: int, group: int, zeros: bo
 def medusa_pack_weight_i4(src: torch.Tensor, group: int, dst: torch.Tensor, dst_rows: int, tile_offset: int = 0, zeros: bool = False, stream=None) -> None:
     """src [n, k] of bf16 or fp16 -> rows 16 * tile_offset .. of the packed 4-bit matrix dst, quantised in groups of a row's features."""
     shape, dtype, gpu = _rows("src", src)
+    _fits("tile_offset", 64, tile_offset)
     _check(lib().medusa_pack_weight_i4(dtype, _operand("src", src, shape, src.dtype, gpu), shape[0], shape[1], group, int(zeros),
                                        _packed_i4("packed", dst, dst_rows, shape[1], group, zeros, gpu), dst_rows, tile_offset, _stream_of(gpu, stream)))
 
@@ -451,6 +460,7 @@ def medusa_pack_codes_i4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optio
     if codes.dim() != 2 or scales.dtype not in _STORAGE:
         raise MedusaError(-2, f"codes: {tuple(codes.shape)}, scales: {scales.dtype}, expected rows and scales of a storage dtype")
     (n, k), gpu = codes.shape, codes.get_device()
+    _fits("tile_offset", 64, tile_offset)
     packed = _packed_i4("packed", dst, dst_rows, k, group, zeros is not None, gpu)
     groups = (n, -(-k // group))
     _check(lib().medusa_pack_codes_i4(_STORAGE[scales.dtype], _operand("codes", codes, (n, k), torch.uint8, gpu), _operand("scales", scales, groups, scales.dtype, gpu),
