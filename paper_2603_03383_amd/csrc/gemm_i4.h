@@ -535,7 +535,8 @@ static int launch_i4_tiles(const I4Product& p, const I4Plan& plan, hipStream_t s
     if (plan.mt == MT && plan.nt == NT && plan.xr == XR && plan.waves == NW)                           \
       return launch_i4_few<E, G, ZEROS, GATED, MT, NT, XR, NW, D, DX, WPE>(p, st);
 #define MDZ_I4_ROWS(MT, NT, NW, WPE) \
-  if (plan.mt == MT && plan.nt == NT && plan.xr == 0 && plan.waves == NW) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, NW, WPE>(p, st);
+  if constexpr (i4_built(I4Plan{MT, NT, NW, 0}, kKind, GATED)) \
+    if (plan.mt == MT && plan.nt == NT && plan.xr == 0 && plan.waves == NW) return launch_i4_rows<E, G, ZEROS, GATED, MT, NT, NW, WPE>(p, st);
   MDZ_I4_CASES
   MDZ_FAIL(MDZ_EINVAL, "linear_i4: no kernel of %d x %d tiles", plan.mt, plan.nt);
 }

@@ -66,7 +66,7 @@ constexpr int i4_kind(bool f16, int groups_of_block, bool zeros) {
 }
 // The cuts for more than 16 rows: for how many rows, rows and tiles (of each matrix, if gated; 0: not gated) of a workgroup, blocks of features of a turn, and a
 // turn's us on a full chip by kind: with one workgroup on a CU, and with two (0: the kernel of few rows, one).  A us of 0: the kind's registers spill, and other cuts are
-// faster wherever this one would do.
+// faster wherever this one would do (256 columns with bf16 zero points in groups of 64 took 1.85 and 4.1 us, which 128 columns with 1.22 and 1.55 beat at every size).
 struct I4Cut {
   I4Plan plan;
   int least_rows, most_rows, rows, tiles, gate_tiles, features;
@@ -80,14 +80,15 @@ constexpr I4Cut kI4Cuts[] = {
     {{4, 2, 8, 16}, 33, 1 << 30, 64, 2, 1, 8, {3.05f, 0.f, 0.f, 3.3f, 0.f, 0.f, 3.17f, 0.f}, {}},
     {{4, 6, 4, 16}, 33, 1 << 30, 64, 6, 3, 4, {3.05f, 3.7f, 0.f, 3.7f, 0.f, 0.f, 4.0f, 0.f}, {}},
     {{4, 2, 4, 0}, 17, 1 << 30, 64, 8, 4, 1, {0.95f, 1.0f, 1.16f, 1.15f, 1.22f, 1.54f, 1.04f, 1.2f}, {1.2f, 1.25f, 1.53f, 1.36f, 1.55f, 2.0f, 1.46f, 1.67f}},
-    {{4, 4, 4, 0}, 17, 1 << 30, 64, 16, 8, 1, {1.38f, 1.43f, 2.05f, 1.55f, 1.85f, 2.43f, 1.69f, 2.07f}, {2.12f, 2.35f, 2.87f, 2.33f, 4.1f, 3.42f, 2.65f, 3.1f}},
+    {{4, 4, 4, 0}, 17, 1 << 30, 64, 16, 8, 1, {1.38f, 1.43f, 2.05f, 1.55f, 0.f, 2.43f, 1.69f, 2.07f}, {2.12f, 2.35f, 2.87f, 2.33f, 0.f, 3.42f, 2.65f, 3.1f}},
 };
-// Whether the kernel of few rows has this cut for this kind.  Up to 16 rows groups of 32 take two tiles at most, with eight waves where zero points cost registers.
+// Whether there is a kernel with this cut for this kind.  Up to 16 rows groups of 32 take two tiles at most, with eight waves where zero points cost registers.
 constexpr bool i4_built(const I4Plan& plan, int kind, bool gated) {
   const bool of_32 = kind == 2 || kind == 5 || kind == 7;
+  if (plan.mt == 1 && gated && !of_32 && plan.nt == 2 && plan.waves == 4 && plan.xr == 4) return false;  // (9 to 16 rows of a gated product: four tiles beyond one per CU)
   if (plan.mt == 1) return !(of_32 && plan.nt == 4) && !(kind == 5 && plan.nt == 2 && plan.waves == 4) && (gated || kind == 5 || !(plan.nt == 2 && plan.waves == 8));
   for (const I4Cut& c : kI4Cuts)
-    if (c.plan.xr != 0 && c.plan.mt == plan.mt && c.plan.nt == plan.nt) return c.us[kind] > 0.f;
+    if (c.plan.mt == plan.mt && c.plan.nt == plan.nt && c.plan.waves == plan.waves && c.plan.xr == plan.xr) return c.us[kind] > 0.f;
   return false;
 }
 
