@@ -217,9 +217,10 @@ __device__ inline void finish_i4(const I4Product& p, const f32x4_t (&tot)[NT][MT
 // A workgroup of NW waves makes 16 MT rows x NT tiles of 16 columns (GATED: NT / 2 of each matrix); the waves share out the blocks of
 // features, so each streams contiguous weights, and their sums meet in LDS.  A wave's rows of X pass through LDS of its own, which turns whole
 // lines of memory into operands; no wave waits for another before the end.  XR: pieces of four rows that are loaded (4 MT, or fewer).
-// Bound by the stream of weights at few rows: 1 x 12288 x 4096 in 8.6 us, 3.0 TB/s with the launch and the first loads in it, gated 1 x 11008 x 4096 13.2, 3.5 TB/s (registers
-// hold 4 to 8 blocks per wave ahead; LDS would add a step that few rows do not need).  At 64 rows by loads, LDS, conversions and products one after the other:
-// 64 x 4096 x 4096 9.9 us, gated 64 x 11008 x 4096 24.2, where the ring below takes 31 and 32 (32 and 172 workgroups).
+// Bound by the stream of weights at few rows: 1 x 12288 x 4096 in 8.5 us, 3.0 TB/s with the launch and the first loads in it, gated 1 x 11008 x 4096 12.9, 3.6 TB/s (registers
+// hold 4 to 8 blocks per wave ahead; LDS would add a step that few rows do not need).  At 64 rows by loads, LDS, conversions and products one after the other, with all of X
+// through every workgroup: 64 x 4096 x 4096 9.7 us, gated 64 x 11008 x 4096 24.1, where the ring below takes 31 and 32 (32 and 172 workgroups).  With one tile to a wave
+// half of the products are those that make the sums of x.
 template <typename E, int G, bool ZEROS, bool GATED, int MT, int NT, int XR, int NW, int D, int DX, int WPE>
 __global__ void __launch_bounds__(NW * 64, WPE) gemm_i4_kernel(I4Product p) {
   typedef I4Stream<E, G, ZEROS, GATED, NT> Stream;
@@ -350,9 +351,10 @@ done:
 // everyone's, and behind it the place of the turn that all have read is requested anew.  Two turns, so that a CU has two workgroups or three: their phases of
 // loads, LDS reads, conversions and products then overlap.  (One workgroup of eight waves and three turns, all in step: gated 1024 x 11008 x 4096 219 us
 // where two of four waves take 200, 64 x 128000 x 4096 85 and 81.)
-// Bound by the matrix cores and the vector units, which convert codes and scale sums: gated 1024 x 11008 x 4096 in 194-204 us (0.90-0.95 PFLOP/s; each is busy for half of the
-// clocks, and they overlap little), gated 200 x 12800 x 4096 in groups of 64 with zero points 88, 64 x 128000 x 4096 87 (3.6 TB/s).  64 rows to a wave, so that a
-// converted tile serves four products; 256 columns to four waves, or 128 where that fills the CUs better (kI4Cuts).
+// Bound by the matrix cores and the vector units, which convert codes and scale sums: gated 1024 x 11008 x 4096 in 189-195 us (0.95-0.98 PFLOP/s; each is busy for half of the
+// clocks, and they overlap little), gated 200 x 12800 x 4096 in groups of 64 with zero points 86-88, 64 x 128000 x 4096 84-86 (3.6 TB/s).  A fifth of the matrix cores' clocks are
+// the sums of x, which each wave makes for itself (sum_block).  64 rows to a wave, so that a converted tile serves four products; 256 columns to four waves, or
+// 128 where that fills the CUs better (kI4Cuts).
 template <int G, bool ZEROS, bool GATED, int MT, int NT, int NW>
 struct I4Ring {
   static constexpr int kRows = MT * 16, kMats = GATED ? 2 : 1, kTiles = NW * NT / kMats;  // tiles of each matrix

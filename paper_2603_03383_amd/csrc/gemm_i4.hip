@@ -12,7 +12,8 @@ struct I4Source {
   const void* scales;
   const uint8_t* zeros;
 };
-// Bound by memory: 128000 x 4096 codes in 209 us, 3.8 TB/s in and out, with 8-byte loads and 32-bit divisions (988 us with single bytes and 64-bit ones).
+// Codes are bound by memory: 128000 x 4096 in 210 us, 3.8 TB/s in and out, with 8-byte loads and 32-bit divisions (988 us with single bytes and 64-bit ones).  Quantising, once
+// when a model is loaded, is bound by the threads' way over their group by single elements: 128000 x 4096 of bf16 in groups of 128 4.8 ms, 4096 x 4096 148 us.
 template <typename E>
 __global__ void __launch_bounds__(256) pack_i4_kernel(I4Source s, int64_t n_rows, int k, int group, bool with_zeros, uint32_t* __restrict__ codes,
                                                       E* __restrict__ scales, uint8_t* __restrict__ zeros, uint32_t blocks, int64_t words) {
